@@ -658,6 +658,136 @@ repops_status_t repops_gelu_erf_backward(const repops_order_t *order, int64_t n,
                                          const float *dY, float *dX, const repops_launch_t *launch,
                                          void *hip_stream);
 
+/* ------------------------------------------------------------------------
+ * Generation step: what runs around the products when a Llama program (Section
+ * 4.2) generates tokens -- the residual addition with its norm, products of
+ * 8-bit operands and the drawing of a token.  8-bit codes are symmetric with one
+ * scale per row: a code q in [-127, 127] stands for q * scale.
+ * ------------------------------------------------------------------------ */
+
+/*
+ * repops_add_rmsnorm_rows -- residual addition, RMSNorm of the sum and, where
+ * wanted, the 8-bit codes of its output:
+ *     s_j = RN(x_j + r_j) (s = x if R is NULL);
+ *     ms, rstd, y_j as repops_rmsnorm_rows computes them from s;
+ *     scale = RN(max |y_j| / 127);  q_j = rint(RN(y_j / scale)) (ties to even),
+ *     clamped to +-127.  scale = 0 gives codes 0.  A row with a y that is not
+ *     finite gets scale NaN and codes 0.
+ *   X, ldx; R, ldr     rows x cols; R may be NULL.
+ *   S, lds             NULL or output for the sum.
+ *   Y, ldy             NULL or output for y.
+ *   Q, ldq; scale      both NULL, or outputs: codes (ldq >= cols, in bytes) and
+ *                      [rows] scales.
+ *   gamma, eps, rstd_out, order, launch   as for repops_rmsnorm_rows; the launch
+ *                      never changes an output.
+ *   At least one of S, Y, Q (REPOPS_ERR_NULL).  S and Y may each coincide exactly
+ *   with X or with R; no other overlap of an output with an input or with
+ *   another output is allowed (REPOPS_ERR_ALIAS).
+ */
+repops_status_t repops_add_rmsnorm_rows(const repops_order_t *order, int64_t rows, int64_t cols,
+                                        const float *X, int64_t ldx, const float *R, int64_t ldr,
+                                        const float *gamma, float eps, float *S, int64_t lds,
+                                        float *Y, int64_t ldy, int8_t *Q, int64_t ldq,
+                                        float *scale, float *rstd_out,
+                                        const repops_launch_t *launch, void *hip_stream);
+
+/*
+ * repops_add_rmsnorm_backward_rows -- gradients of repops_add_rmsnorm_rows (S
+ * and Y) from its S and rstd.  dY is the gradient of Y and dS that of S by its
+ * other uses (the residual stream), or NULL:
+ *     dx_j = RN(dx'_j + ds_j), dx' and dgamma as repops_rmsnorm_backward_rows
+ *     computes them from S and dY (dx = dx' if dS is NULL).
+ *   dX is the gradient of X and, the same values, of R.
+ *   Arguments, workspace (repops_rmsnorm_backward_workspace), aliasing and launch
+ *   as for repops_rmsnorm_backward_rows; dX may also coincide exactly with dS.
+ */
+repops_status_t repops_add_rmsnorm_backward_rows(
+    const repops_order_t *order, int64_t rows, int64_t cols, const float *S, int64_t lds,
+    const float *dY, int64_t lddy, const float *dS, int64_t ldds, const float *rstd,
+    const float *gamma, float *dX, int64_t lddx, float *dgamma, void *workspace,
+    uint64_t workspace_bytes, const repops_launch_t *launch, void *hip_stream);
+
+/*
+ * repops_quantize_rows -- 8-bit codes and scales of rows, as
+ * repops_add_rmsnorm_rows takes them of its y: the layout of a weight for
+ * repops_matmul_q8 (one scale per output feature) or of activations.
+ *   X, ldx  rows x cols;  Q, ldq >= cols (bytes), scale [rows]: outputs, which
+ *   overlap neither X nor each other.  cols = 0 gives scales +0.
+ *   The largest magnitude is the same in any order: there is no order
+ *   descriptor.  launch: NULL or AUTO.
+ */
+repops_status_t repops_quantize_rows(int64_t rows, int64_t cols, const float *X, int64_t ldx,
+                                     int8_t *Q, int64_t ldq, float *scale,
+                                     const repops_launch_t *launch, void *hip_stream);
+
+/*
+ * repops_matmul_q8 -- product of 8-bit operands with scales (Section 3.2's
+ * contraction over integers):
+ *     acc = sum over kk of A[i][kk] * B[j][kk], exact in 32-bit integers;
+ *     C[i][j] = RN(RN(RN(acc) * a_scale[i]) * b_scale[j])  (+ bias[j], one
+ *     rounded addition), RN to binary32.
+ *   Integer sums are exact, so every order gives the same bits: there is no order
+ *   descriptor.  Any code in [-128, 127] is taken.
+ *   A, lda    m x k, A[i][kk] at A[i*lda + kk] (lda >= k, in bytes).
+ *   B, ldb    n x k, B[j][kk] at B[j*ldb + kk] (ldb >= k): a weight stored with
+ *             one row per output feature, as repops_quantize_rows leaves it.
+ *   a_scale   [m];  b_scale [n];  bias NULL or [n].
+ *   C, ldc    m x n output, ldc >= n, overlapping no input.
+ *   k <= REPOPS_Q8_MAX_K, where a sum of products of -128 still fits; k = 0 gives
+ *   acc = 0.  launch: NULL or AUTO.
+ */
+#define REPOPS_Q8_MAX_K 131071
+repops_status_t repops_matmul_q8(int64_t m, int64_t n, int64_t k, const int8_t *A, int64_t lda,
+                                 const float *a_scale, const int8_t *B, int64_t ldb,
+                                 const float *b_scale, const float *bias, float *C, int64_t ldc,
+                                 const repops_launch_t *launch, void *hip_stream);
+
+/* Workspace bytes of repops_sample_rows. */
+repops_status_t repops_sample_workspace(int64_t rows, int64_t vocab, uint64_t *bytes);
+
+/*
+ * repops_sample_rows -- one token per row of logits from a given random number.
+ * Every step is exact or one fixed sequence, so a row's token depends on nothing
+ * but its inputs.  With m the row's largest logit:
+ *     it = 1 / temperature;  d_j = (l_j - m) * it in binary64 (0 where l_j = m);
+ *     w_j = rint(exp(d_j) * 2^43), an integer: 0 for d_j <= -31, else
+ *         n = rint(d * log2(e));  r = fma(n, -ln2_hi, d);  r = fma(n, -ln2_lo, r);
+ *         p = Horner over 1/i!, i = 11..0, with fma;  w = rint(p * 2^(n + 43)).
+ *   The tokens are taken in order of descending logit, equal ones by ascending
+ *   index (-0 and +0 are equal).  Each filter keeps a prefix of that order, the
+ *   first token always; the shortest prefix holds:
+ *     top_k   the first top_k tokens; off where top_k <= 0 or >= vocab.
+ *     top_p   the tokens whose predecessors weigh less than
+ *             ceil(top_p * W), W the weight that top_k leaves; off where
+ *             top_p >= 1 or NaN, the first token alone where top_p <= 0.
+ *     min_p   the tokens with d_j >= log(min_p) (log in binary64 by
+ *             2 atanh((f - 1) / (f + 1)), f in [sqrt(1/2), sqrt(2)), ten terms by
+ *             Horner with fma, plus e ln2); off where min_p <= 0 or NaN; min_p >= 1
+ *             keeps the largest logits.
+ *   With W_kept the weight kept and t = floor(u * W_kept) (u below 0 or NaN counts
+ *   as 0; t at most W_kept - 1), the token is the one at which the running sum of
+ *   weights in that order first exceeds t, and prob = RN(w / W_kept).
+ *   temperature <= 0 or NaN: the first token of the order, with prob 1.
+ *   Masked logits are -infinity: never drawn.  A row without a token (all
+ *   -infinity, or vocab = 0) gives token -1 and prob 0; a row holding a NaN gives
+ *   token -1 and prob NaN.
+ *   L, ldl       rows x vocab logits, ldl >= vocab; vocab <= 2^20.
+ *   u            [rows], uniform in [0, 1).
+ *   temperature, top_p, min_p ([rows] float), top_k ([rows] int32): device
+ *                arrays, each NULL for 1 or off.
+ *   token        [rows] int32 output;  prob NULL or [rows] output.  Outputs
+ *                overlap neither an input nor each other nor the workspace.
+ *   workspace    device memory of at least repops_sample_workspace bytes, 8-byte
+ *                aligned (REPOPS_ERR_STRIDE), contents on return unspecified; calls
+ *                that may overlap in time need one each.
+ *   launch       NULL or AUTO.
+ */
+repops_status_t repops_sample_rows(int64_t rows, int64_t vocab, const float *L, int64_t ldl,
+                                   const float *u, const float *temperature, const int32_t *top_k,
+                                   const float *top_p, const float *min_p, int32_t *token,
+                                   float *prob, void *workspace, uint64_t workspace_bytes,
+                                   const repops_launch_t *launch, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -20,7 +20,11 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
 SOURCES = ["api.cpp", "gemm.hip", "gemm_mfma.hip",
-           "gemm_split.hip", "rows.hip", "elementwise.hip", "train.hip", "llama.hip", "commit.hip"]
+           "gemm_split.hip", "rows.hip", "elementwise.hip", "train.hip", "llama.hip", "commit.hip",
+           "addnorm.hip", "sample.hip"]
+# Sources whose matrix instructions sum integers, exactly and so in any order;
+# the ones above add one rounded floating product at a time.
+INTEGER_SOURCES = ["gemm_q8.hip"]
 
 FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall",
@@ -44,7 +48,7 @@ def _compile(src: str) -> str:
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD_DIR, exist_ok=True)
     with concurrent.futures.ThreadPoolExecutor(max_workers=4) as ex:
-        objs = list(ex.map(_compile, SOURCES))
+        objs = list(ex.map(_compile, SOURCES + INTEGER_SOURCES))
     tmp = LIB_PATH + ".tmp"
     cmd = [HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)

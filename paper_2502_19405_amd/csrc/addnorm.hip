@@ -1,0 +1,286 @@
+// Residual addition with RMSNorm, and the 8-bit row quantiser, for gfx950.
+//
+// s = x + r; ms = rowsum(fma(s, s, .)) / n in the descriptor's row order;
+// rstd = 1 / sqrt(ms + eps); y = RN(s rstd) gamma: the sequence of
+// repops_rmsnorm_rows on the rounded sum, so y has its bits.  The codes of y
+// (quantize.h) leave in the same pass: with a scale per row the values stay in
+// registers between the maximum and the division.
+//
+// Bound: memory.  8 B read and 4 (S) + 4 (Y) or 1 (codes) B written per
+// element; the sum never goes out and back for the norm to read it.
+#include <hip/hip_runtime.h>
+
+#include "generation_internal.h"
+#include "quantize.h"
+#include "row_reduce.h"
+#include "rows_internal.h"
+#include "stream_store.h"
+
+#pragma clang fp contract(off)
+
+namespace repops {
+namespace {
+
+// The columns j0 + 64 t (t < T) of one row: sums into v, all loads issued
+// before any arithmetic, +0 past the row.
+template <int T>
+__device__ __forceinline__ void load_sums(const AddNormArgs& a, int64_t row, int64_t j0,
+                                          float (&v)[T]) {
+  const float* x = a.X + row * a.ldx;
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    const int64_t j = j0 + kWave * t;
+    v[t] = 0.0f;
+    if (j < a.cols) v[t] = x[j];
+  }
+  if (a.R) {
+    const float* r = a.R + row * a.ldr;
+    float rv[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      const int64_t j = j0 + kWave * t;
+      rv[t] = 0.0f;
+      if (j < a.cols) rv[t] = r[j];
+    }
+#pragma unroll
+    for (int t = 0; t < T; ++t) v[t] = v[t] + rv[t];
+  }
+}
+
+template <int T>
+__device__ __forceinline__ void store_sums(const AddNormArgs& a, int64_t row, int64_t j0,
+                                           const float (&v)[T]) {
+  float* s = a.S + row * a.lds;
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    const int64_t j = j0 + kWave * t;
+    if (j < a.cols) st_stream(s + j, v[t]);
+  }
+}
+
+// v becomes y, and is stored where Y is wanted.
+template <int T>
+__device__ __forceinline__ void finish_rows(const AddNormArgs& a, int64_t row, int64_t j0,
+                                            float rstd, float (&v)[T]) {
+#pragma unroll
+  for (int t = 0; t < T; ++t) v[t] = v[t] * rstd;
+  if (a.gamma) {
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      const int64_t j = j0 + kWave * t;
+      if (j < a.cols) v[t] = v[t] * a.gamma[j];
+    }
+  }
+  if (a.Y) {
+    float* y = a.Y + row * a.ldy;
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      const int64_t j = j0 + kWave * t;
+      if (j < a.cols) st_stream(y + j, v[t]);
+    }
+  }
+}
+
+template <int T>
+__device__ __forceinline__ uint32_t lane_max(const AddNormArgs& a, int64_t j0,
+                                             const float (&v)[T]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    const uint32_t b = j0 + kWave * t < a.cols ? mag_bits(v[t]) : 0u;
+    m = b > m ? b : m;
+  }
+  return m;
+}
+
+template <int T>
+__device__ __forceinline__ void store_codes(const AddNormArgs& a, int64_t row, int64_t j0,
+                                            float scale, const float (&v)[T]) {
+  int8_t* q = a.Q + row * a.ldq;
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    const int64_t j = j0 + kWave * t;
+    if (j < a.cols) q[j] = static_cast<int8_t>(quant_code(v[t], scale));
+  }
+}
+
+template <int T>
+__global__ __launch_bounds__(512) void addnorm_wave_kernel(AddNormArgs a, int wpb) {
+  const int lane = threadIdx.x & (kWave - 1);
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * wpb + wave_id();
+  if (row >= a.rows) return;
+  float v[T];
+  load_sums<T>(a, row, lane, v);
+  if (a.S) store_sums<T>(a, row, lane, v);
+  float q = 0.0f;
+#pragma unroll
+  for (int t = 0; t < T; ++t) q = __builtin_fmaf(v[t], v[t], q);  // past the row: fma(0, 0, q) = q
+  const float ms = wave_tree_sum(q) / static_cast<float>(a.cols);
+  const float rstd = 1.0f / __builtin_sqrtf(ms + a.eps);
+  finish_rows<T>(a, row, lane, rstd, v);
+  if (a.Q) {
+    const float scale = quant_scale(wave_max_bits(lane_max<T>(a, lane, v)));
+    store_codes<T>(a, row, lane, scale, v);
+    if (lane == 0) a.scale[row] = scale;
+  }
+  if (lane == 0 && a.rstd_out) a.rstd_out[row] = rstd;
+}
+
+// Wide rows: one row per workgroup of S waves, wave w holding the columns
+// lane + 64 (w T + t); the lanes' chains pass from wave to wave in order, so
+// the bits are those of one wave.
+template <int T>
+__global__ __launch_bounds__(512) void addnorm_split_kernel(AddNormArgs a) {
+  __shared__ float chain[kWave];
+  __shared__ uint32_t wave_top[8];
+  const int lane = threadIdx.x & (kWave - 1);
+  const int w = wave_id();
+  const int S = static_cast<int>(blockDim.x >> 6);
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const int64_t j0 = lane + int64_t(kWave) * T * w;
+    float v[T];
+    load_sums<T>(a, row, j0, v);
+    if (a.S) store_sums<T>(a, row, j0, v);
+    const float q = chain_across_waves(chain, lane, w, S, [&](float c) {
+#pragma unroll
+      for (int t = 0; t < T; ++t) c = __builtin_fmaf(v[t], v[t], c);  // past the row: c
+      return c;
+    });
+    const float ms = wave_tree_sum(q) / static_cast<float>(a.cols);
+    const float rstd = 1.0f / __builtin_sqrtf(ms + a.eps);
+    finish_rows<T>(a, row, j0, rstd, v);
+    if (a.Q) {
+      const uint32_t top = wave_max_bits(lane_max<T>(a, j0, v));
+      if (lane == 0) wave_top[w] = top;
+      __syncthreads();
+      uint32_t m = 0;
+      for (int k = 0; k < S; ++k) m = wave_top[k] > m ? wave_top[k] : m;
+      const float scale = quant_scale(m);
+      store_codes<T>(a, row, j0, scale, v);
+      if (w == 0 && lane == 0) a.scale[row] = scale;
+    }
+    if (w == 0 && lane == 0 && a.rstd_out) a.rstd_out[row] = rstd;
+    __syncthreads();  // every wave has read the chains and maxima before the next row
+  }
+}
+
+// Any order descriptor and any width: one wave per row, the row read again for
+// each step.  An element's outputs are written by the lane that reads it last.
+__global__ __launch_bounds__(64) void addnorm_generic_kernel(AddNormArgs a) {
+  __shared__ float qs[1024];
+  const int lane = threadIdx.x;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const float* x = a.X + row * a.ldx;
+    const float* r = a.R ? a.R + row * a.ldr : nullptr;
+    auto sum_at = [&](int64_t j) { return r ? x[j] + r[j] : x[j]; };
+    auto sq_term = [&](float q, int64_t j) {
+      const float s = sum_at(j);
+      return __builtin_fmaf(s, s, q);
+    };
+    const float ms =
+        generic_row_sum(a.cols, a.W, a.blocked, sq_term, qs) / static_cast<float>(a.cols);
+    const float rstd = 1.0f / __builtin_sqrtf(ms + a.eps);
+    auto y_of = [&](float s, int64_t j) {
+      const float t = s * rstd;
+      return a.gamma ? t * a.gamma[j] : t;
+    };
+    float scale = 0.0f;
+    if (a.Q) {
+      uint32_t m = 0;
+      for (int64_t j = lane; j < a.cols; j += kWave) {
+        const uint32_t b = mag_bits(y_of(sum_at(j), j));
+        m = b > m ? b : m;
+      }
+      scale = quant_scale(wave_max_bits(m));
+      if (lane == 0) a.scale[row] = scale;
+    }
+    for (int64_t j = lane; j < a.cols; j += kWave) {
+      const float s = sum_at(j);
+      const float y = y_of(s, j);
+      if (a.S) st_stream(a.S + row * a.lds + j, s);
+      if (a.Y) st_stream(a.Y + row * a.ldy + j, y);
+      if (a.Q) a.Q[row * a.ldq + j] = static_cast<int8_t>(quant_code(y, scale));
+    }
+    if (lane == 0 && a.rstd_out) a.rstd_out[row] = rstd;
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------------------
+// 8-bit codes of rows: one workgroup per row, the row read for its maximum and
+// again for its codes.
+// ---------------------------------------------------------------------------
+
+__global__ __launch_bounds__(256) void quantize_kernel(QuantArgs a) {
+  __shared__ uint32_t wave_top[4];
+  const int tid = threadIdx.x;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const float* x = a.X + row * a.ldx;
+    int8_t* q = a.Q + row * a.ldq;
+    uint32_t m = 0;
+    for (int64_t j = tid; j < a.cols; j += 256) {
+      const uint32_t b = mag_bits(x[j]);
+      m = b > m ? b : m;
+    }
+    m = wave_max_bits(m);
+    if ((tid & 63) == 0) wave_top[tid >> 6] = m;
+    __syncthreads();
+    for (int k = 0; k < 4; ++k) m = wave_top[k] > m ? wave_top[k] : m;
+    const float scale = quant_scale(m);
+    for (int64_t j = tid; j < a.cols; j += 256) q[j] = static_cast<int8_t>(quant_code(x[j], scale));
+    if (tid == 0) a.scale[row] = scale;
+    __syncthreads();
+  }
+}
+
+using WaveKernel = void (*)(AddNormArgs, int);
+WaveKernel pick_wave(int64_t cols) {
+  if (cols <= kWave * 1) return addnorm_wave_kernel<1>;
+  if (cols <= kWave * 2) return addnorm_wave_kernel<2>;
+  if (cols <= kWave * 4) return addnorm_wave_kernel<4>;
+  if (cols <= kWave * 8) return addnorm_wave_kernel<8>;
+  if (cols <= kWave * 12) return addnorm_wave_kernel<12>;
+  if (cols <= kWave * 16) return addnorm_wave_kernel<16>;
+  if (cols <= kWave * 32) return addnorm_wave_kernel<32>;
+  return addnorm_wave_kernel<64>;
+}
+
+unsigned row_blocks(int64_t rows) {
+  const int64_t cap = int64_t(1) << 22;  // workgroups loop over the rows beyond
+  return static_cast<unsigned>(rows < cap ? rows : cap);
+}
+
+}  // namespace
+
+hipError_t launch_addnorm_wave(const AddNormArgs& a, int wpb, hipStream_t s) {
+  const int64_t blocks = (a.rows + wpb - 1) / wpb;
+  hipLaunchKernelGGL(pick_wave(a.cols), dim3(static_cast<unsigned>(blocks)), dim3(kWave * wpb), 0,
+                     s, a, wpb);
+  return hipGetLastError();
+}
+
+hipError_t launch_addnorm_split(const AddNormArgs& a, int S, hipStream_t s) {
+  const int64_t per_wave = (a.cols + int64_t(kWave) * S - 1) / (int64_t(kWave) * S);
+  void (*k)(AddNormArgs) = nullptr;
+  if (per_wave <= 1) k = addnorm_split_kernel<1>;
+  else if (per_wave <= 2) k = addnorm_split_kernel<2>;
+  else if (per_wave <= 4) k = addnorm_split_kernel<4>;
+  else if (per_wave <= 8) k = addnorm_split_kernel<8>;
+  else if (per_wave <= 16) k = addnorm_split_kernel<16>;
+  else if (per_wave <= 32) k = addnorm_split_kernel<32>;
+  else return hipErrorInvalidValue;
+  hipLaunchKernelGGL(k, dim3(row_blocks(a.rows)), dim3(kWave * S), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_addnorm_generic(const AddNormArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(addnorm_generic_kernel, dim3(row_blocks(a.rows)), dim3(kWave), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_quantize(const QuantArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(quantize_kernel, dim3(row_blocks(a.rows)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace repops

@@ -10,6 +10,7 @@
 #include "train_internal.h"
 #include "llama_internal.h"
 #include "commit_internal.h"
+#include "generation_internal.h"
 #include "rows_internal.h"
 
 using repops::AdamScalars;
@@ -878,12 +879,14 @@ repops_status_t repops_layernorm_backward_workspace(const repops_order_t* order,
   return REPOPS_OK;
 }
 
-// LayerNorm and RMSNorm backward (rms: no mean input, no dbeta).
+// LayerNorm and RMSNorm backward (rms: no mean input, no dbeta); dS (nullable)
+// is added to dX.
 static repops_status_t norm_backward(
     bool rms, const repops_order_t* order, int64_t rows, int64_t cols, const float* X,
     int64_t ldx, const float* dY, int64_t lddy, const float* mean, const float* rstd,
     const float* gamma, float* dX, int64_t lddx, float* dgamma, float* dbeta, void* workspace,
-    uint64_t workspace_bytes, const repops_launch_t* launch, void* hip_stream) {
+    uint64_t workspace_bytes, const repops_launch_t* launch, void* hip_stream,
+    const float* dS = nullptr, int64_t ldds = 0) {
   if (!order_valid(order)) return REPOPS_ERR_ORDER;
   if (rows < 0 || cols < 0 || rows > kMaxDim || cols > (int64_t(1) << 24)) return REPOPS_ERR_SHAPE;
   if (rows > 0 && cols == 0) return REPOPS_ERR_SHAPE;
@@ -903,20 +906,25 @@ static repops_status_t norm_backward(
   if (need > 0 && (!workspace || workspace_bytes < need)) return REPOPS_ERR_WORKSPACE;
   // Inputs and outputs as (extent, base, leading dimension).  No output may
   // overlap another output or an input, except that dX may coincide exactly
-  // with X or with dY.
+  // with X, with dY or with dS.
   struct Span {
     Extent e;
     const float* base;
     int64_t ld;
   };
-  Span in[5], out[4];
-  int nin = 0, nout = 0;
+  Span in[6], out[4];
+  int nin = 0, nout = 0, places = 2;  // the first `places` inputs are those dX may replace
   if (rows > 0) {
     if ((st = check_matrix(X, rows, cols, ldx)) != REPOPS_OK) return st;
     if ((st = check_matrix(dY, rows, cols, lddy)) != REPOPS_OK) return st;
+    if (dS && (st = check_matrix(dS, rows, cols, ldds)) != REPOPS_OK) return st;
     if ((!rms && !mean) || !rstd) return REPOPS_ERR_NULL;
     in[nin++] = {extent_of(X, 1, 0, 1, 0, rows, cols, ldx), X, ldx};
     in[nin++] = {extent_of(dY, 1, 0, 1, 0, rows, cols, lddy), dY, lddy};
+    if (dS) {
+      in[nin++] = {extent_of(dS, 1, 0, 1, 0, rows, cols, ldds), dS, ldds};
+      places = 3;
+    }
     if (!rms) in[nin++] = {vec_extent(mean, rows), mean, rows};
     in[nin++] = {vec_extent(rstd, rows), rstd, rows};
   }
@@ -938,7 +946,7 @@ static repops_status_t norm_backward(
     for (int j = 0; j < nin; ++j) {
       const bool is_dx = dX && rows > 0 && i == 0;
       const bool exact = out[i].base == in[j].base && out[i].ld == in[j].ld;
-      if (is_dx && j < 2 && exact) continue;  // dX in place of X or dY
+      if (is_dx && j < places && exact) continue;  // dX in place of X, dY or dS
       if (overlaps(out[i].e, in[j].e)) return REPOPS_ERR_ALIAS;
     }
   }
@@ -955,6 +963,7 @@ static repops_status_t norm_backward(
   a.blocked = order->row_combine == REPOPS_ROW_BLOCKED_LTR;
   a.mean = mean; a.rstd = rstd; a.gamma = gamma;
   a.rms = rms ? 1 : 0;
+  a.dS = dS; a.ldds = ldds;
   // Both gradients on the wave path with row blocks: one fused pass over X
   // and dY (R rows staged per pass: the launch's waves per block, else a
   // choice by size).
@@ -1321,6 +1330,193 @@ repops_status_t repops_gelu_erf_backward(const repops_order_t* order, int64_t n,
   if (st != REPOPS_OK || n == 0) return st;
   return hip_status(repops::launch_gelu_bwd(n, X, dY, dX, threads, max_blocks,
                                             static_cast<hipStream_t>(hip_stream), true));
+}
+
+// ---------------------------------------------------------------------------
+// Generation step
+// ---------------------------------------------------------------------------
+
+// Byte range of `rows` rows of `cols` elements of `size` bytes.
+static Extent byte_extent(const void* p, int64_t rows, int64_t cols, int64_t ld, int64_t size) {
+  const uintptr_t b = reinterpret_cast<uintptr_t>(p);
+  if (rows <= 0 || cols <= 0) return {b, b};
+  return {b, b + static_cast<uintptr_t>(((rows - 1) * ld + cols) * size)};
+}
+
+// An operand for the overlap checks: no output may overlap another output, or an
+// input unless both may coincide and do so exactly.
+struct Operand {
+  Extent e;
+  const void* base;
+  int64_t ld;
+  bool may_coincide;
+};
+static bool outputs_clash(const Operand* out, int nout, const Operand* in, int nin) {
+  for (int i = 0; i < nout; ++i) {
+    for (int j = i + 1; j < nout; ++j)
+      if (overlaps(out[i].e, out[j].e)) return true;
+    for (int j = 0; j < nin; ++j) {
+      if (out[i].may_coincide && in[j].may_coincide && out[i].base == in[j].base &&
+          out[i].ld == in[j].ld)
+        continue;
+      if (overlaps(out[i].e, in[j].e)) return true;
+    }
+  }
+  return false;
+}
+
+// Addresses one past any row stay in range: (rows - 1) * ld + cols elements of
+// `size` bytes within 2^62.
+static bool span_fits(int64_t rows, int64_t cols, int64_t ld, int64_t size) {
+  const __int128 last = static_cast<__int128>(rows > 0 ? rows - 1 : 0) * ld + cols;
+  return last * size < (static_cast<__int128>(1) << 62);
+}
+
+static bool auto_launch(const repops_launch_t* l) {
+  return !l || (l->kind == REPOPS_LAUNCH_AUTO && launch_params_zero_from(l, 0));
+}
+
+repops_status_t repops_add_rmsnorm_rows(const repops_order_t* order, int64_t rows, int64_t cols,
+                                        const float* X, int64_t ldx, const float* R, int64_t ldr,
+                                        const float* gamma, float eps, float* S, int64_t lds,
+                                        float* Y, int64_t ldy, int8_t* Q, int64_t ldq,
+                                        float* scale, float* rstd_out,
+                                        const repops_launch_t* launch, void* hip_stream) {
+  if (!order_valid(order)) return REPOPS_ERR_ORDER;
+  if (rows < 0 || cols < 0 || rows > kMaxDim || cols > (int64_t(1) << 24)) return REPOPS_ERR_SHAPE;
+  if (rows > 0 && cols == 0) return REPOPS_ERR_SHAPE;
+  uint32_t kind;
+  int wpb, split;
+  repops_status_t st =
+      row_launch_kind(order, launch, cols, &kind, &wpb, repops::rmsnorm_wave_max_cols(), &split,
+                      repops::rmsnorm_split_max_cols, 8);
+  if (st != REPOPS_OK || rows == 0) return st;
+  if (!X || (!S && !Y && !Q) || (!Q != !scale)) return REPOPS_ERR_NULL;
+  Operand in[3], out[5];
+  int nin = 0, nout = 0;
+  auto matrix = [&](Operand* list, int* n, const void* p, int64_t ld, int64_t size, bool coincide) {
+    if (ld < cols) st = REPOPS_ERR_STRIDE;
+    else if (!span_fits(rows, cols, ld, size)) st = REPOPS_ERR_SHAPE;
+    list[(*n)++] = {byte_extent(p, rows, cols, ld, size), p, ld, coincide};
+  };
+  auto vector = [&](Operand* list, int* n, const void* p, int64_t count) {
+    list[(*n)++] = {byte_extent(p, 1, count, count, 4), p, count, false};
+  };
+  matrix(in, &nin, X, ldx, 4, true);
+  if (R) matrix(in, &nin, R, ldr, 4, true);
+  if (gamma) vector(in, &nin, gamma, cols);
+  if (S) matrix(out, &nout, S, lds, 4, true);
+  if (Y) matrix(out, &nout, Y, ldy, 4, true);
+  if (Q) matrix(out, &nout, Q, ldq, 1, false);
+  if (scale) vector(out, &nout, scale, rows);
+  if (rstd_out) vector(out, &nout, rstd_out, rows);
+  if (st != REPOPS_OK) return st;
+  if (outputs_clash(out, nout, in, nin)) return REPOPS_ERR_ALIAS;
+  repops::AddNormArgs a{};
+  a.rows = rows; a.cols = cols; a.X = X; a.ldx = ldx; a.R = R; a.ldr = ldr;
+  a.gamma = gamma; a.eps = eps; a.S = S; a.lds = lds; a.Y = Y; a.ldy = ldy;
+  a.Q = Q; a.ldq = ldq; a.scale = scale; a.rstd_out = rstd_out;
+  a.W = static_cast<int>(order->row_width);
+  a.blocked = order->row_combine == REPOPS_ROW_BLOCKED_LTR;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  if (kind == REPOPS_LAUNCH_ROWS_WAVE && split > 1)
+    return hip_status(repops::launch_addnorm_split(a, split, s));
+  // (rows beyond a launch's thread limit loop in the generic kernel: the same bits)
+  if (kind == REPOPS_LAUNCH_ROWS_WAVE && (rows + wpb - 1) / wpb <= repops::max_workgroups(64 * wpb))
+    return hip_status(repops::launch_addnorm_wave(a, wpb, s));
+  return hip_status(repops::launch_addnorm_generic(a, s));
+}
+
+repops_status_t repops_add_rmsnorm_backward_rows(
+    const repops_order_t* order, int64_t rows, int64_t cols, const float* S, int64_t lds,
+    const float* dY, int64_t lddy, const float* dS, int64_t ldds, const float* rstd,
+    const float* gamma, float* dX, int64_t lddx, float* dgamma, void* workspace,
+    uint64_t workspace_bytes, const repops_launch_t* launch, void* hip_stream) {
+  return norm_backward(true, order, rows, cols, S, lds, dY, lddy, nullptr, rstd, gamma, dX, lddx,
+                       dgamma, nullptr, workspace, workspace_bytes, launch, hip_stream, dS, ldds);
+}
+
+repops_status_t repops_quantize_rows(int64_t rows, int64_t cols, const float* X, int64_t ldx,
+                                     int8_t* Q, int64_t ldq, float* scale,
+                                     const repops_launch_t* launch, void* hip_stream) {
+  if (rows < 0 || cols < 0 || rows > kMaxDim || cols > kMaxDim) return REPOPS_ERR_SHAPE;
+  if (!auto_launch(launch)) return REPOPS_ERR_LAUNCH;
+  if (rows == 0) return REPOPS_OK;
+  if (!scale || (cols > 0 && (!X || !Q))) return REPOPS_ERR_NULL;
+  if (ldx < cols || ldq < cols) return REPOPS_ERR_STRIDE;
+  if (!span_fits(rows, cols, ldx, 4) || !span_fits(rows, cols, ldq, 1)) return REPOPS_ERR_SHAPE;
+  const Operand in = {byte_extent(X, rows, cols, ldx, 4), X, ldx, false};
+  const Operand out[2] = {{byte_extent(Q, rows, cols, ldq, 1), Q, ldq, false},
+                          {byte_extent(scale, 1, rows, rows, 4), scale, rows, false}};
+  if (outputs_clash(out, 2, &in, 1)) return REPOPS_ERR_ALIAS;
+  repops::QuantArgs a{rows, cols, X, ldx, Q, ldq, scale};
+  return hip_status(repops::launch_quantize(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+repops_status_t repops_matmul_q8(int64_t m, int64_t n, int64_t k, const int8_t* A, int64_t lda,
+                                 const float* a_scale, const int8_t* B, int64_t ldb,
+                                 const float* b_scale, const float* bias, float* C, int64_t ldc,
+                                 const repops_launch_t* launch, void* hip_stream) {
+  if (m < 0 || n < 0 || k < 0 || m > kMaxDim || n > kMaxDim || k > REPOPS_Q8_MAX_K)
+    return REPOPS_ERR_SHAPE;
+  if (!auto_launch(launch)) return REPOPS_ERR_LAUNCH;
+  if (m == 0 || n == 0) return REPOPS_OK;
+  if (!C || !a_scale || !b_scale || (k > 0 && (!A || !B))) return REPOPS_ERR_NULL;
+  if (ldc < n || (k > 0 && (lda < k || ldb < k))) return REPOPS_ERR_STRIDE;
+  if (!span_fits(m, n, ldc, 4) || (k > 0 && (!span_fits(m, k, lda, 1) || !span_fits(n, k, ldb, 1))))
+    return REPOPS_ERR_SHAPE;
+  Operand in[5];
+  int nin = 0;
+  in[nin++] = {byte_extent(a_scale, 1, m, m, 4), a_scale, m, false};
+  in[nin++] = {byte_extent(b_scale, 1, n, n, 4), b_scale, n, false};
+  if (k > 0) {
+    in[nin++] = {byte_extent(A, m, k, lda, 1), A, lda, false};
+    in[nin++] = {byte_extent(B, n, k, ldb, 1), B, ldb, false};
+  }
+  if (bias) in[nin++] = {byte_extent(bias, 1, n, n, 4), bias, n, false};
+  const Operand out = {byte_extent(C, m, n, ldc, 4), C, ldc, false};
+  if (outputs_clash(&out, 1, in, nin)) return REPOPS_ERR_ALIAS;
+  repops::Q8Args a{m, n, k, A, lda, B, ldb, a_scale, b_scale, bias, C, ldc};
+  return hip_status(repops::launch_matmul_q8(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+repops_status_t repops_sample_workspace(int64_t rows, int64_t vocab, uint64_t* bytes) {
+  if (!bytes) return REPOPS_ERR_NULL;
+  if (rows < 0 || vocab < 0 || rows > kMaxDim || vocab > repops::kSampleMaxVocab)
+    return REPOPS_ERR_SHAPE;
+  *bytes = repops::sample_workspace_bytes(rows, vocab);
+  return REPOPS_OK;
+}
+
+repops_status_t repops_sample_rows(int64_t rows, int64_t vocab, const float* L, int64_t ldl,
+                                   const float* u, const float* temperature, const int32_t* top_k,
+                                   const float* top_p, const float* min_p, int32_t* token,
+                                   float* prob, void* workspace, uint64_t workspace_bytes,
+                                   const repops_launch_t* launch, void* hip_stream) {
+  uint64_t need = 0;
+  repops_status_t st = repops_sample_workspace(rows, vocab, &need);
+  if (st != REPOPS_OK) return st;
+  if (!auto_launch(launch)) return REPOPS_ERR_LAUNCH;
+  if (rows == 0) return REPOPS_OK;
+  if (!u || !token || (vocab > 0 && !L)) return REPOPS_ERR_NULL;
+  if (ldl < vocab) return REPOPS_ERR_STRIDE;
+  if (!span_fits(rows, vocab, ldl, 4)) return REPOPS_ERR_SHAPE;
+  if (need > 0 && (!workspace || workspace_bytes < need)) return REPOPS_ERR_WORKSPACE;
+  if (need > 0 && reinterpret_cast<uintptr_t>(workspace) % 8 != 0) return REPOPS_ERR_STRIDE;
+  Operand in[6], out[3];
+  int nin = 0, nout = 0;
+  in[nin++] = {byte_extent(L, rows, vocab, ldl, 4), L, ldl, false};
+  for (const void* p : {static_cast<const void*>(u), static_cast<const void*>(temperature),
+                        static_cast<const void*>(top_k), static_cast<const void*>(top_p),
+                        static_cast<const void*>(min_p)})
+    if (p) in[nin++] = {byte_extent(p, 1, rows, rows, 4), p, rows, false};
+  out[nout++] = {byte_extent(token, 1, rows, rows, 4), token, rows, false};
+  if (prob) out[nout++] = {byte_extent(prob, 1, rows, rows, 4), prob, rows, false};
+  if (need > 0)
+    out[nout++] = {byte_extent(workspace, 1, static_cast<int64_t>(need), 0, 1), workspace, 0, false};
+  if (outputs_clash(out, nout, in, nin)) return REPOPS_ERR_ALIAS;
+  repops::SampleArgs a{rows, vocab, L, ldl, u, temperature, top_k, top_p, min_p, token, prob};
+  return hip_status(repops::launch_sample(a, workspace, static_cast<hipStream_t>(hip_stream)));
 }
 
 // ---------------------------------------------------------------------------

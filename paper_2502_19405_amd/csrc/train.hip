@@ -162,14 +162,38 @@ __device__ __forceinline__ void ln_bwd_terms(const RowBwdArgs& a, const float* x
   }
 }
 
+// The ADD forms' values of dS in the columns j0 + 64 t of one row, read ahead of
+// the row's reductions (+0 past the row); nothing otherwise.
+template <int T, bool ADD>
+struct AddRow {
+  float v[ADD ? T : 1];
+  __device__ __forceinline__ void load(const RowBwdArgs& a, int64_t row, int64_t j0) {
+    if constexpr (ADD) {
+      const float* ds = a.dS + row * a.ldds;
+#pragma unroll
+      for (int t = 0; t < T; ++t) {
+        const int64_t j = j0 + kWave * t;
+        v[t] = 0.0f;
+        if (j < a.cols) v[t] = ds[j];
+      }
+    }
+  }
+  __device__ __forceinline__ float operator()(int t, float dx) const {
+    if constexpr (ADD) return dx + v[t];
+    else return dx;
+  }
+};
+
 // dX of one row by one wave (row < a.rows, uniform over the wave; all 64
 // lanes active).
-template <int T>
+template <int T, bool ADD>
 __device__ __forceinline__ void layernorm_bwd_row(const RowBwdArgs& a, int64_t row, int lane) {
   const float* x = a.Y + row * a.ldy;
   const float* dy = a.dY + row * a.lddy;
   float* dx = a.dX + row * a.lddx;
   const float mean = a.rms ? 0.0f : a.mean[row], rstd = a.rstd[row];
+  AddRow<T, ADD> add;
+  add.load(a, row, lane);
   float tv[T], gv[T];
   ln_bwd_terms<T>(a, x, dy, lane, mean, rstd, tv, gv);
   float q = 0.0f;
@@ -186,7 +210,7 @@ __device__ __forceinline__ void layernorm_bwd_row(const RowBwdArgs& a, int64_t r
     const float u = gv[t] - am;
     const float tb = tv[t] * bm;
     const float w = u - tb;
-    return rstd * w;
+    return add(t, rstd * w);
   };
   if (a.cols == kWave * T) {
 #pragma unroll
@@ -200,12 +224,12 @@ __device__ __forceinline__ void layernorm_bwd_row(const RowBwdArgs& a, int64_t r
   }
 }
 
-template <int T>
+template <int T, bool ADD>
 __global__ __launch_bounds__(512) void layernorm_bwd_wave_kernel(RowBwdArgs a, int wpb) {
   const int lane = threadIdx.x & (kWave - 1);
   const int64_t row = static_cast<int64_t>(blockIdx.x) * wpb + wave_id();
   if (row >= a.rows) return;
-  layernorm_bwd_row<T>(a, row, lane);
+  layernorm_bwd_row<T, ADD>(a, row, lane);
 }
 
 // ---------------------------------------------------------------------------
@@ -259,7 +283,7 @@ __global__ __launch_bounds__(512) void softmax_bwd_split_kernel(RowBwdArgs a) {
   }
 }
 
-template <int T>
+template <int T, bool ADD>
 __global__ __launch_bounds__(512) void layernorm_bwd_split_kernel(RowBwdArgs a) {
   __shared__ float chain_g[kWave];
   __shared__ float chain_gt[kWave];
@@ -273,6 +297,8 @@ __global__ __launch_bounds__(512) void layernorm_bwd_split_kernel(RowBwdArgs a) 
     float* dx = a.dX + row * a.lddx;
     const float mean = a.rms ? 0.0f : a.mean[row], rstd = a.rstd[row];
     const int64_t j0 = lane + int64_t(kWave) * T * w;
+    AddRow<T, ADD> add;
+    add.load(a, row, j0);
     float tv[T], gv[T];
     ln_bwd_terms<T>(a, x, dy, j0, mean, rstd, tv, gv);
     float am = 0.0f;
@@ -297,7 +323,7 @@ __global__ __launch_bounds__(512) void layernorm_bwd_split_kernel(RowBwdArgs a) 
       if (j < a.cols) {
         const float u = gv[t] - am;
         const float tb = tv[t] * bm;
-        st_stream(dx + j, rstd * (u - tb));
+        st_stream(dx + j, add(t, rstd * (u - tb)));
       }
     }
     __syncthreads();  // chains read before the next row
@@ -327,7 +353,9 @@ __global__ __launch_bounds__(64) void layernorm_bwd_generic_kernel(RowBwdArgs a)
       const float u = gj - am;
       const float tb = tj * bm;
       const float w = u - tb;
-      st_stream(dx + j, rstd * w);  // dX may equal X or dY: element j is read before it is written
+      const float d = rstd * w;
+      // dX may equal X, dY or dS: element j is read before it is written
+      st_stream(dx + j, a.dS ? d + a.dS[row * a.ldds + j] : d);
     }
     __syncthreads();
   }
@@ -512,7 +540,7 @@ __global__ __launch_bounds__(NT) void layernorm_param_combine_kernel(LnParamArgs
 
 constexpr int kFusedChains = 4;  // columns per thread in the chain phase
 
-template <int T, int MAXT, bool PF>
+template <int T, int MAXT, bool PF, bool ADD>
 __global__ __launch_bounds__(MAXT) void layernorm_bwd_fused_kernel(RowBwdArgs a, LnParamArgs p,
                                                                    int R, int64_t nblk) {
   extern __shared__ float stage[];  // [R][cols] t, then [R][cols] dy
@@ -566,6 +594,8 @@ __global__ __launch_bounds__(MAXT) void layernorm_bwd_fused_kernel(RowBwdArgs a,
       if (!PF) load_row(row);
       float* dx = a.dX + row * a.lddx;
       const float mean = a.rms ? 0.0f : a.mean[row], rstd = a.rstd[row];
+      AddRow<T, ADD> add;
+      add.load(a, row, lane);
       float tv[T], gv[T];
       float q = 0.0f;
 #pragma unroll
@@ -595,7 +625,7 @@ __global__ __launch_bounds__(MAXT) void layernorm_bwd_fused_kernel(RowBwdArgs a,
           const float u = gv[t] - am;
           const float tb = tv[t] * bm;
           const float wv = u - tb;
-          st_stream(dx + j, rstd * wv);
+          st_stream(dx + j, add(t, rstd * wv));
         }
       }
       if (PF && row + R < r1) load_row(row + R);  // next row in flight through the barriers and chains
@@ -657,7 +687,7 @@ constexpr int kSplitWaves = 8;
 // the results are the same bits.  Every wave takes part in every step (the
 // steps hold workgroup barriers); a group past end works on row first and
 // stores nothing.
-template <int T, int S>
+template <int T, int S, bool ADD>
 __device__ __forceinline__ void layernorm_bwd_rows_grouped(const RowBwdArgs& a, int64_t first,
                                                            int64_t stride, int64_t end, int lane,
                                                            int w) {
@@ -682,6 +712,8 @@ __device__ __forceinline__ void layernorm_bwd_rows_grouped(const RowBwdArgs& a, 
     const float* dy = a.dY + rr * a.lddy;
     const float mean = a.rms ? 0.0f : a.mean[rr], rstd = a.rstd[rr];
     const int64_t j0 = lane + int64_t(kWave) * T * h;
+    AddRow<T, ADD> add;
+    add.load(a, rr, j0);
     float tv[T], gv[T];
     ln_bwd_terms<T>(a, x, dy, j0, mean, rstd, tv, gv);
     float am = 0.0f;
@@ -708,7 +740,7 @@ __device__ __forceinline__ void layernorm_bwd_rows_grouped(const RowBwdArgs& a, 
         if (j < a.cols) {
           const float u = gv[t] - am;
           const float tb = tv[t] * bm;
-          st_stream(dx + j, rstd * (u - tb));
+          st_stream(dx + j, add(t, rstd * (u - tb)));
         }
       }
     }
@@ -723,7 +755,7 @@ __device__ __forceinline__ void layernorm_bwd_rows_grouped(const RowBwdArgs& a, 
 // one wave measured faster than two of 16).
 constexpr int kColsplitGroupT = 16;
 
-template <int T, int SWU>
+template <int T, int SWU, bool ADD>
 __global__ __launch_bounds__(kSplitWaves * kWave) void layernorm_bwd_colsplit_kernel(
     RowBwdArgs a, LnParamArgs p, int G, int slice, int64_t nblk) {
   constexpr int SW = kWave * SWU;            // LDS pitch: slice columns at most
@@ -780,12 +812,12 @@ __global__ __launch_bounds__(kSplitWaves * kWave) void layernorm_bwd_colsplit_ke
     static_assert(T % kColsplitGroupT == 0 && kSplitWaves % (T / kColsplitGroupT) == 0,
                   "row groups must tile the workgroup");
     constexpr int S = T / kColsplitGroupT, P = kSplitWaves / S;
-    layernorm_bwd_rows_grouped<kColsplitGroupT, S>(a, r0 + int64_t(g) * P, int64_t(P) * G, r1,
-                                                   lane, w);
+    layernorm_bwd_rows_grouped<kColsplitGroupT, S, ADD>(a, r0 + int64_t(g) * P, int64_t(P) * G, r1,
+                                                        lane, w);
   } else {
     const int64_t stride = int64_t(kSplitWaves) * G;
     for (int64_t row = r0 + int64_t(g) * kSplitWaves + w; row < r1; row += stride)
-      layernorm_bwd_row<T>(a, row, lane);
+      layernorm_bwd_row<T, ADD>(a, row, lane);
   }
 
   float pg = 0.0f, pb = 0.0f;
@@ -930,15 +962,16 @@ WaveBwdKernel pick_softmax_bwd(int64_t cols) {
   return softmax_bwd_wave_kernel<64>;
 }
 
+template <bool ADD>
 WaveBwdKernel pick_layernorm_bwd(int64_t cols) {
-  if (cols <= kWave * 1) return layernorm_bwd_wave_kernel<1>;
-  if (cols <= kWave * 2) return layernorm_bwd_wave_kernel<2>;
-  if (cols <= kWave * 4) return layernorm_bwd_wave_kernel<4>;
-  if (cols <= kWave * 8) return layernorm_bwd_wave_kernel<8>;
-  if (cols <= kWave * 12) return layernorm_bwd_wave_kernel<12>;
-  if (cols <= kWave * 16) return layernorm_bwd_wave_kernel<16>;
-  if (cols <= kWave * 32) return layernorm_bwd_wave_kernel<32>;
-  return layernorm_bwd_wave_kernel<64>;
+  if (cols <= kWave * 1) return layernorm_bwd_wave_kernel<1, ADD>;
+  if (cols <= kWave * 2) return layernorm_bwd_wave_kernel<2, ADD>;
+  if (cols <= kWave * 4) return layernorm_bwd_wave_kernel<4, ADD>;
+  if (cols <= kWave * 8) return layernorm_bwd_wave_kernel<8, ADD>;
+  if (cols <= kWave * 12) return layernorm_bwd_wave_kernel<12, ADD>;
+  if (cols <= kWave * 16) return layernorm_bwd_wave_kernel<16, ADD>;
+  if (cols <= kWave * 32) return layernorm_bwd_wave_kernel<32, ADD>;
+  return layernorm_bwd_wave_kernel<64, ADD>;
 }
 
 using SplitBwdKernel = void (*)(RowBwdArgs);
@@ -955,7 +988,8 @@ SplitBwdKernel pick_split_bwd(int64_t cols, int S) {
   return nullptr;
 }
 template <int T> struct SoftmaxBwdSplit { static constexpr SplitBwdKernel fn = softmax_bwd_split_kernel<T>; };
-template <int T> struct LayernormBwdSplit { static constexpr SplitBwdKernel fn = layernorm_bwd_split_kernel<T>; };
+template <int T> struct LayernormBwdSplit { static constexpr SplitBwdKernel fn = layernorm_bwd_split_kernel<T, false>; };
+template <int T> struct LayernormAddBwdSplit { static constexpr SplitBwdKernel fn = layernorm_bwd_split_kernel<T, true>; };
 
 hipError_t launch_split_bwd(SplitBwdKernel k, const RowBwdArgs& a, int S, hipStream_t s) {
   if (!k) return hipErrorInvalidValue;
@@ -969,14 +1003,15 @@ using FusedKernel = void (*)(RowBwdArgs, LnParamArgs, int, int64_t);
 
 // Kernels for R <= 8 waves (512 threads); the widest rows (32 values per
 // lane) load each row at the top of its pass instead of one pass ahead.
+template <bool ADD>
 FusedKernel pick_layernorm_fused(int64_t cols) {
-  if (cols <= kWave * 1) return layernorm_bwd_fused_kernel<1, 512, true>;
-  if (cols <= kWave * 2) return layernorm_bwd_fused_kernel<2, 512, true>;
-  if (cols <= kWave * 4) return layernorm_bwd_fused_kernel<4, 512, true>;
-  if (cols <= kWave * 8) return layernorm_bwd_fused_kernel<8, 512, true>;
-  if (cols <= kWave * 12) return layernorm_bwd_fused_kernel<12, 512, true>;
-  if (cols <= kWave * 16) return layernorm_bwd_fused_kernel<16, 512, true>;
-  return layernorm_bwd_fused_kernel<32, 512, false>;
+  if (cols <= kWave * 1) return layernorm_bwd_fused_kernel<1, 512, true, ADD>;
+  if (cols <= kWave * 2) return layernorm_bwd_fused_kernel<2, 512, true, ADD>;
+  if (cols <= kWave * 4) return layernorm_bwd_fused_kernel<4, 512, true, ADD>;
+  if (cols <= kWave * 8) return layernorm_bwd_fused_kernel<8, 512, true, ADD>;
+  if (cols <= kWave * 12) return layernorm_bwd_fused_kernel<12, 512, true, ADD>;
+  if (cols <= kWave * 16) return layernorm_bwd_fused_kernel<16, 512, true, ADD>;
+  return layernorm_bwd_fused_kernel<32, 512, false, ADD>;
 }
 
 unsigned row_grid(int64_t rows) {
@@ -1012,7 +1047,8 @@ hipError_t launch_softmax_bwd_generic(const RowBwdArgs& a, hipStream_t s) {
 
 hipError_t launch_layernorm_bwd_wave(const RowBwdArgs& a, int wpb, hipStream_t s) {
   const int64_t blocks = (a.rows + wpb - 1) / wpb;
-  hipLaunchKernelGGL(pick_layernorm_bwd(a.cols), dim3(static_cast<unsigned>(blocks)),
+  const WaveBwdKernel k = a.dS ? pick_layernorm_bwd<true>(a.cols) : pick_layernorm_bwd<false>(a.cols);
+  hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(blocks)),
                      dim3(kWave * wpb), 0, s, a, wpb);
   return hipGetLastError();
 }
@@ -1022,7 +1058,9 @@ hipError_t launch_softmax_bwd_split(const RowBwdArgs& a, int S, hipStream_t s) {
 }
 
 hipError_t launch_layernorm_bwd_split(const RowBwdArgs& a, int S, hipStream_t s) {
-  return launch_split_bwd(pick_split_bwd<LayernormBwdSplit>(a.cols, S), a, S, s);
+  const SplitBwdKernel k = a.dS ? pick_split_bwd<LayernormAddBwdSplit>(a.cols, S)
+                                : pick_split_bwd<LayernormBwdSplit>(a.cols, S);
+  return launch_split_bwd(k, a, S, s);
 }
 
 hipError_t launch_layernorm_bwd_generic(const RowBwdArgs& a, hipStream_t s) {
@@ -1098,7 +1136,9 @@ hipError_t launch_layernorm_bwd_fused(const RowBwdArgs& a, const LnParamArgs& p,
                                       hipStream_t s) {
   const int64_t nblk = layernorm_param_blocks(a.rows, p.k_block);
   const size_t lds = sizeof(float) * 2 * static_cast<size_t>(R) * static_cast<size_t>(a.cols);
-  hipLaunchKernelGGL(pick_layernorm_fused(a.cols), dim3(static_cast<unsigned>(nblk)),
+  const FusedKernel k =
+      a.dS ? pick_layernorm_fused<true>(a.cols) : pick_layernorm_fused<false>(a.cols);
+  hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(nblk)),
                      dim3(R * kWave), lds, s, a, p, R, nblk);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || nblk == 1) return e;
@@ -1107,16 +1147,24 @@ hipError_t launch_layernorm_bwd_fused(const RowBwdArgs& a, const LnParamArgs& p,
 
 using ColsplitKernel = void (*)(RowBwdArgs, LnParamArgs, int, int, int64_t);
 
-template <int SWU>
+template <int SWU, bool ADD>
 ColsplitKernel pick_colsplit_t(int64_t cols) {
-  if (cols <= kWave * 1) return layernorm_bwd_colsplit_kernel<1, SWU>;
-  if (cols <= kWave * 2) return layernorm_bwd_colsplit_kernel<2, SWU>;
-  if (cols <= kWave * 4) return layernorm_bwd_colsplit_kernel<4, SWU>;
-  if (cols <= kWave * 8) return layernorm_bwd_colsplit_kernel<8, SWU>;
-  if (cols <= kWave * 12) return layernorm_bwd_colsplit_kernel<12, SWU>;
-  if (cols <= kWave * 16) return layernorm_bwd_colsplit_kernel<16, SWU>;
-  if (cols <= kWave * 32) return layernorm_bwd_colsplit_kernel<32, SWU>;
-  return layernorm_bwd_colsplit_kernel<64, SWU>;
+  if (cols <= kWave * 1) return layernorm_bwd_colsplit_kernel<1, SWU, ADD>;
+  if (cols <= kWave * 2) return layernorm_bwd_colsplit_kernel<2, SWU, ADD>;
+  if (cols <= kWave * 4) return layernorm_bwd_colsplit_kernel<4, SWU, ADD>;
+  if (cols <= kWave * 8) return layernorm_bwd_colsplit_kernel<8, SWU, ADD>;
+  if (cols <= kWave * 12) return layernorm_bwd_colsplit_kernel<12, SWU, ADD>;
+  if (cols <= kWave * 16) return layernorm_bwd_colsplit_kernel<16, SWU, ADD>;
+  if (cols <= kWave * 32) return layernorm_bwd_colsplit_kernel<32, SWU, ADD>;
+  return layernorm_bwd_colsplit_kernel<64, SWU, ADD>;
+}
+
+template <bool ADD>
+ColsplitKernel pick_colsplit(int64_t cols, int swu) {
+  return swu == 1   ? pick_colsplit_t<1, ADD>(cols)
+         : swu == 2 ? pick_colsplit_t<2, ADD>(cols)
+         : swu == 3 ? pick_colsplit_t<3, ADD>(cols)
+                    : pick_colsplit_t<4, ADD>(cols);
 }
 
 bool layernorm_colsplit_plan(int64_t rows, int64_t cols, int64_t k_block, ColsplitPlan* pl) {
@@ -1141,10 +1189,8 @@ bool layernorm_colsplit_plan(int64_t rows, int64_t cols, int64_t k_block, Colspl
 hipError_t launch_layernorm_bwd_colsplit(const RowBwdArgs& a, const LnParamArgs& p,
                                          const ColsplitPlan& pl, hipStream_t s) {
   const int64_t nblk = layernorm_param_blocks(a.rows, p.k_block);
-  ColsplitKernel k = pl.swu == 1   ? pick_colsplit_t<1>(a.cols)
-                     : pl.swu == 2 ? pick_colsplit_t<2>(a.cols)
-                     : pl.swu == 3 ? pick_colsplit_t<3>(a.cols)
-                                   : pick_colsplit_t<4>(a.cols);
+  const ColsplitKernel k =
+      a.dS ? pick_colsplit<true>(a.cols, pl.swu) : pick_colsplit<false>(a.cols, pl.swu);
   hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(nblk * pl.G)), dim3(kSplitWaves * kWave), 0,
                      s, a, p, pl.G, pl.slice, nblk);
   hipError_t e = hipGetLastError();

@@ -22,6 +22,9 @@ struct RowBwdArgs {
   int64_t period;     // softmax causal period, 0 = none
   const float* mean; const float* rstd; const float* gamma;
   int rms;            // RMSNorm: no mean, no a term
+  // Nullable (LayerNorm / RMSNorm): a gradient added to dX by the kernels' ADD
+  // forms, the residual stream's in the backward of addition and norm.
+  const float* dS; int64_t ldds;
 };
 
 hipError_t launch_softmax_bwd_wave(const RowBwdArgs& a, int waves_per_block, hipStream_t s);

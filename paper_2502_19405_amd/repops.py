@@ -141,6 +141,17 @@ _SIGNATURES = {
     "repops_gelu_erf_backward": (_i32, [_op, _i64, _vp, _vp, _vp, _lp, _vp]),
     "repops_commit_workspace": (_i32, [ctypes.c_uint64, _u32, ctypes.POINTER(ctypes.c_uint64)]),
     "repops_commit": (_i32, [_vp, ctypes.c_uint64, _u32, _vp, _vp, ctypes.c_uint64, _lp, _vp]),
+    "repops_add_rmsnorm_rows": (_i32, [_op, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _f32, _vp, _i64,
+                                       _vp, _i64, _vp, _i64, _vp, _vp, _lp, _vp]),
+    "repops_add_rmsnorm_backward_rows": (_i32, [_op, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64,
+                                                _vp, _vp, _vp, _i64, _vp, _vp, ctypes.c_uint64,
+                                                _lp, _vp]),
+    "repops_quantize_rows": (_i32, [_i64, _i64, _vp, _i64, _vp, _i64, _vp, _lp, _vp]),
+    "repops_matmul_q8": (_i32, [_i64, _i64, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _vp, _i64,
+                                _lp, _vp]),
+    "repops_sample_workspace": (_i32, [_i64, _i64, ctypes.POINTER(ctypes.c_uint64)]),
+    "repops_sample_rows": (_i32, [_i64, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                  ctypes.c_uint64, _lp, _vp]),
 }
 EXPORTS = tuple(_SIGNATURES)
 
@@ -851,6 +862,222 @@ def swiglu_backward(G: torch.Tensor, Up: torch.Tensor, dY: torch.Tensor,
                                        _launch(launch), _stream(G))
     _check(rc, "repops_swiglu_backward")
     return dG, dU
+
+
+# ---------------------------------------------------------------------------
+# generation step: addition with norm, 8-bit products, drawing tokens
+# ---------------------------------------------------------------------------
+
+Q8_MAX_K = 131071  # REPOPS_Q8_MAX_K
+_I8, _I32 = torch.int8, torch.int32
+
+
+def _same_device(*tensors):
+    """The library is given addresses: all of a call's tensors must be on one device."""
+    dev = None
+    for t in tensors:
+        if t is not None:
+            if dev is None:
+                dev = t.device
+            elif t.device != dev:
+                raise ValueError(f"tensors on different devices: {dev} and {t.device}")
+
+
+def _typed(t: torch.Tensor, dtype, name: str):
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {str(dtype)[6:]}")
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    return t.data_ptr()
+
+
+def _row_values(t, name: str, rows: int, dtype=_F32):
+    """Pointer of an optional contiguous [rows] device vector."""
+    if t is None:
+        return None
+    if t.shape != (rows,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous [{rows}] tensor")
+    return _typed(t, dtype, name)
+
+
+def _row_major(t: torch.Tensor, name: str):
+    """_rows, for matrices that may be empty or one column wide, whose column
+    stride says nothing."""
+    if t.dim() == 2 and (t.numel() == 0 or t.shape[1] == 1):
+        rows, cols = t.shape
+        return rows, cols, max(t.stride(0) if rows > 1 and cols else cols, 1)
+    return _rows(t, name)
+
+
+def _shaped(t: torch.Tensor, rows: int, cols: int, name: str) -> int:
+    """Row stride of a [rows, cols] matrix."""
+    if t.shape != (rows, cols):
+        raise ValueError(f"{name} must be [{rows}, {cols}] (got {list(t.shape)})")
+    return _row_major(t, name)[2]
+
+
+def _add_rmsnorm(X, R, gamma, eps, order, launch, S, Y, Q, scale, rstd_out):
+    rows, cols, ldx = _row_major(X, "X")
+    _same_device(X, R, gamma, S, Y, Q, scale, rstd_out)
+    opt = lambda t, name: (None, 0) if t is None else (  # noqa: E731
+        _dev(t, name), _shaped(t, rows, cols, name))
+    pr, ldr = opt(R, "R")
+    ps, lds = opt(S, "sum_out")
+    py, ldy = opt(Y, "out")
+    pq, ldq = (None, 0) if Q is None else (_typed(Q, _I8, "q_out"), _shaped(Q, rows, cols, "q_out"))
+    rc = (_lib or load()).repops_add_rmsnorm_rows(
+        _ord(order), rows, cols, _dev(X, "X"), ldx, pr, ldr, _vec(gamma, "gamma", cols), float(eps),
+        ps, lds, py, ldy, pq, ldq, _row_values(scale, "scale_out", rows),
+        _row_values(rstd_out, "rstd_out", rows), _launch(launch), _stream(X))
+    _check(rc, "repops_add_rmsnorm_rows")
+
+
+def add_rmsnorm_rows(X: torch.Tensor, R: torch.Tensor | None = None,
+                     gamma: torch.Tensor | None = None, eps: float = 1e-5,
+                     order: Order | None = None, launch: Launch | None = None,
+                     sum_out: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                     rstd_out: torch.Tensor | None = None):
+    """(S, Y) with S = X + R and Y = rmsnorm_rows(S, gamma, eps) from one pass.
+    R None: Y is the norm of X, and S is X itself unless sum_out is given.  sum_out
+    and out may each be X or R."""
+    if sum_out is None and R is not None:
+        sum_out = torch.empty_like(X, memory_format=torch.contiguous_format)
+    if out is None:
+        out = torch.empty_like(X, memory_format=torch.contiguous_format)
+    _add_rmsnorm(X, R, gamma, eps, order, launch, sum_out, out, None, None, rstd_out)
+    return X if sum_out is None else sum_out, out
+
+
+def add_rmsnorm_quantize_rows(X: torch.Tensor, R: torch.Tensor | None = None,
+                              gamma: torch.Tensor | None = None, eps: float = 1e-5,
+                              order: Order | None = None, launch: Launch | None = None,
+                              sum_out: torch.Tensor | None = None,
+                              q_out: torch.Tensor | None = None,
+                              scale_out: torch.Tensor | None = None,
+                              out: torch.Tensor | None = None,
+                              rstd_out: torch.Tensor | None = None):
+    """(S, Q, scale): S as add_rmsnorm_rows gives it, and the codes (int8) and
+    scales of the Y it gives, which is written only if out is passed."""
+    if sum_out is None and R is not None:
+        sum_out = torch.empty_like(X, memory_format=torch.contiguous_format)
+    if q_out is None:
+        q_out = torch.empty(X.shape, dtype=_I8, device=X.device)
+    if scale_out is None:
+        scale_out = torch.empty(X.shape[:1], dtype=_F32, device=X.device)
+    _add_rmsnorm(X, R, gamma, eps, order, launch, sum_out, out, q_out, scale_out, rstd_out)
+    return X if sum_out is None else sum_out, q_out, scale_out
+
+
+def add_rmsnorm_backward_rows(S: torch.Tensor, dY: torch.Tensor, rstd: torch.Tensor,
+                              gamma: torch.Tensor | None = None, dS: torch.Tensor | None = None,
+                              need_dx: bool = True, need_dgamma: bool = True,
+                              order: Order | None = None, launch: Launch | None = None,
+                              dx_out: torch.Tensor | None = None,
+                              dgamma_out: torch.Tensor | None = None,
+                              workspace: torch.Tensor | None = None):
+    """(dX, dgamma) of add_rmsnorm_rows from its S and rstd; dX is the gradient of
+    X and of R.  dS is the gradient that reaches S by its other uses; dx_out may be
+    S, dY or dS.  Entries not requested are None."""
+    rows, cols, lds = _row_major(S, "S")
+    lddy = _shaped(dY, rows, cols, "dY")
+    _same_device(S, dY, rstd, gamma, dS, dx_out, dgamma_out, workspace)
+    pds, ldds = (None, 0) if dS is None else (_dev(dS, "dS"), _shaped(dS, rows, cols, "dS"))
+    dx = dgamma = None
+    lddx = cols
+    if need_dx:
+        dx = dx_out if dx_out is not None else torch.empty_like(S, memory_format=torch.contiguous_format)
+        lddx = _shaped(dx, rows, cols, "dx_out")
+    wptr, wbytes = None, 0
+    if need_dgamma:
+        dgamma = dgamma_out if dgamma_out is not None else torch.empty(cols, dtype=_F32,
+                                                                       device=S.device)
+        if workspace is None:
+            need = rmsnorm_backward_workspace(rows, cols, order)
+            if need:
+                workspace = torch.empty(need // 4, dtype=_F32, device=S.device)
+        wptr, wbytes = _workspace(workspace)
+    rc = load().repops_add_rmsnorm_backward_rows(
+        _ord(order), rows, cols, _dev(S, "S"), lds, _dev(dY, "dY"), lddy, pds, ldds,
+        _row_values(rstd, "rstd", rows), _vec(gamma, "gamma", cols),
+        None if dx is None else _dev(dx, "dx_out"), lddx, _vec(dgamma, "dgamma_out", cols), wptr,
+        wbytes, _launch(launch), _stream(S))
+    _check(rc, "repops_add_rmsnorm_backward_rows")
+    return dx, dgamma
+
+
+def quantize_rows(X: torch.Tensor, q_out: torch.Tensor | None = None,
+                  scale_out: torch.Tensor | None = None):
+    """(Q, scale): 8-bit codes of X [rows, cols] with a scale per row, X near
+    Q * scale[:, None]."""
+    rows, cols, ldx = _row_major(X, "X")
+    if q_out is None:
+        q_out = torch.empty(X.shape, dtype=_I8, device=X.device)
+    if scale_out is None:
+        scale_out = torch.empty(rows, dtype=_F32, device=X.device)
+    _same_device(X, q_out, scale_out)
+    ldq = _shaped(q_out, rows, cols, "q_out")
+    rc = load().repops_quantize_rows(rows, cols, _dev(X, "X"), ldx, _typed(q_out, _I8, "q_out"), ldq,
+                                     _row_values(scale_out, "scale_out", rows), None, _stream(X))
+    _check(rc, "repops_quantize_rows")
+    return q_out, scale_out
+
+
+def matmul_q8(A: torch.Tensor, a_scale: torch.Tensor, B: torch.Tensor, b_scale: torch.Tensor,
+              bias: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """C [m, n] = (A * a_scale) (B * b_scale)^T (+ bias) of 8-bit codes A [m, k] and
+    B [n, k], row-major, the sums over k exact in integers."""
+    m, k, lda = _row_major(A, "A")
+    n, k2, ldb = _row_major(B, "B")
+    if k != k2:
+        raise ValueError(f"inner dimensions differ: {k} vs {k2}")
+    if out is None:
+        out = torch.empty((m, n), dtype=_F32, device=A.device)
+    _same_device(A, a_scale, B, b_scale, bias, out)
+    ldc = _shaped(out, m, n, "out")
+    rc = (_lib or load()).repops_matmul_q8(
+        m, n, k, _typed(A, _I8, "A"), lda, _row_values(a_scale, "a_scale", m), _typed(B, _I8, "B"),
+        ldb, _row_values(b_scale, "b_scale", n), _row_values(bias, "bias", n), _dev(out, "out"), ldc,
+        None, _stream(out))
+    _check(rc, "repops_matmul_q8")
+    return out
+
+
+def sample_workspace(rows: int, vocab: int) -> int:
+    """Bytes of workspace sample_rows needs."""
+    n = ctypes.c_uint64(0)
+    _check((_lib or load()).repops_sample_workspace(rows, vocab, ctypes.byref(n)),
+           "repops_sample_workspace")
+    return n.value
+
+
+def sample_rows(logits: torch.Tensor, u: torch.Tensor, temperature: torch.Tensor | None = None,
+                top_k: torch.Tensor | None = None, top_p: torch.Tensor | None = None,
+                min_p: torch.Tensor | None = None, token_out: torch.Tensor | None = None,
+                prob_out: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """(token, prob): one token (int32) per row of logits [rows, vocab], drawn with
+    the given u [rows] in [0, 1) from the tokens that the row's filters keep, and its
+    probability among them.  The parameters are [rows] device tensors (top_k int32),
+    None for temperature 1 or a filter that is off; temperature 0 takes the likeliest
+    token.  A row without a token gives -1."""
+    rows, vocab, ldl = _row_major(logits, "logits")
+    if token_out is None:
+        token_out = torch.empty(rows, dtype=_I32, device=logits.device)
+    if prob_out is None:
+        prob_out = torch.empty(rows, dtype=_F32, device=logits.device)
+    if workspace is None:
+        need = sample_workspace(rows, vocab)
+        if need:
+            workspace = torch.empty(need // 8, dtype=torch.int64, device=logits.device)
+    _same_device(logits, u, temperature, top_k, top_p, min_p, token_out, prob_out, workspace)
+    wptr, wbytes = _workspace(workspace)
+    rc = (_lib or load()).repops_sample_rows(
+        rows, vocab, _dev(logits, "logits"), ldl, _row_values(u, "u", rows),
+        _row_values(temperature, "temperature", rows), _row_values(top_k, "top_k", rows, _I32),
+        _row_values(top_p, "top_p", rows), _row_values(min_p, "min_p", rows),
+        _row_values(token_out, "token_out", rows, _I32), _row_values(prob_out, "prob_out", rows),
+        wptr, wbytes, None, _stream(logits))
+    _check(rc, "repops_sample_rows")
+    return token_out, prob_out
 
 
 # ---------------------------------------------------------------------------
