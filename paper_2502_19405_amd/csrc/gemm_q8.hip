@@ -75,13 +75,19 @@ struct Q8Tile {
   static_assert(BM % (RPL * NW) == 0 && BN % (RPL * NW) == 0, "whole loads per wave");
   static_assert(CPR == 4 || CPR == 8, "slices of 64 or 128 codes");
 
-  struct Smem {
-    int8_t a[NS][BM * BK], b[NS][BN * BK];
+  // The output's turning space (see store) takes the slots' place.
+  static constexpr int PITCH = TN + 8;
+  static_assert(PITCH % 16 == 8, "see store");
+  union alignas(16) Smem {
+    struct {
+      int8_t a[NS][BM * BK], b[NS][BN * BK];
+    };
+    int turn[NW][32 * PITCH];
   };
 
   // Where chunk c of row r lies within the row.
   __device__ static __forceinline__ int place(int r, int c) {
-    return CPR == 8 ? c ^ (r & 7) : c ^ ((r >> 1) & 3);
+    return CPR == 8 ? c ^ ((r >> 1) & 7) : c ^ ((r >> 2) & 3);
   }
 
   struct Pack {
@@ -102,22 +108,16 @@ struct Q8Tile {
     }
     return r;
   }
-  __device__ static __forceinline__ void read_pack(const int8_t* sa, const int8_t* sb,
-                                                   const Reads& rd, int q, Pack& pk) {
-#pragma unroll
-    for (int i = 0; i < IM; ++i)
-      pk.a[i] = *reinterpret_cast<const v4i*>(sa + rd.a[q] + i * 32 * BK);
-#pragma unroll
-    for (int j = 0; j < IN; ++j)
-      pk.b[j] = *reinterpret_cast<const v4i*>(sb + rd.b[q] + j * 32 * BK);
+  // Read r of a step's operands (A's first).
+  __device__ static __forceinline__ void read_one(const int8_t* sa, const int8_t* sb,
+                                                  const Reads& rd, int q, int r, Pack& pk) {
+    if (r < IM) pk.a[r] = *reinterpret_cast<const v4i*>(sa + rd.a[q] + r * 32 * BK);
+    else pk.b[r - IM] = *reinterpret_cast<const v4i*>(sb + rd.b[q] + (r - IM) * 32 * BK);
   }
 
-  template <int LO, int HI>
-  __device__ static __forceinline__ void steps(const Pack& pk, v16i (&acc)[IM][IN]) {
-#pragma unroll
-    for (int t = LO; t < HI; ++t)
-      acc[t / IN][t % IN] = __builtin_amdgcn_mfma_i32_32x32x32_i8(pk.a[t / IN], pk.b[t % IN],
-                                                                  acc[t / IN][t % IN], 0, 0, 0);
+  __device__ static __forceinline__ void step(const Pack& pk, int t, v16i (&acc)[IM][IN]) {
+    acc[t / IN][t % IN] = __builtin_amdgcn_mfma_i32_32x32x32_i8(pk.a[t / IN], pk.b[t % IN],
+                                                                acc[t / IN][t % IN], 0, 0, 0);
   }
 
   // Sources of this wave's direct loads: the rows' start, and the lane's first
@@ -146,73 +146,88 @@ struct Q8Tile {
     }
     return s;
   }
-  // Chunks past the last one repeat it: in bounds, and zeroed in A's operands.
-  __device__ static void issue(Smem& sm, const Src& src, int s, int slot, int wave, int last) {
-#pragma unroll
-    for (int u = 0; u < AU; ++u) {
-      const int kk = s * BK + src.ka[u];
-      __builtin_amdgcn_global_load_lds((global_void_ptr)(src.a[u] + (kk < last ? kk : last)),
-                                       (lds_void_ptr)(sm.a[slot] + (wave + u * NW) * 1024), 16, 0,
-                                       0);
-    }
-#pragma unroll
-    for (int u = 0; u < BU; ++u) {
-      const int kk = s * BK + src.kb[u];
-      __builtin_amdgcn_global_load_lds((global_void_ptr)(src.b[u] + (kk < last ? kk : last)),
-                                       (lds_void_ptr)(sm.b[slot] + (wave + u * NW) * 1024), 16, 0,
-                                       0);
-    }
+  // Load u of this wave's share of slice s (A's first).  Chunks past the last one
+  // repeat it: in bounds, and zeroed in A's operands.
+  __device__ static __forceinline__ void issue(Smem& sm, const Src& src, int u, int s, int slot,
+                                               int wave, int last) {
+    const bool is_a = u < AU;
+    const int v = is_a ? u : u - AU;
+    const int kk = s * BK + (is_a ? src.ka[v] : src.kb[v]);
+    const int8_t* row = is_a ? src.a[v] : src.b[v];
+    int8_t* to = (is_a ? sm.a[slot] : sm.b[slot]) + (wave + v * NW) * 1024;
+    __builtin_amdgcn_global_load_lds((global_void_ptr)(row + (kk < last ? kk : last)),
+                                     (lds_void_ptr)to, 16, 0, 0);
   }
 
   // Contraction with direct loads: rows 16-byte aligned, K a positive multiple of
-  // 16.  NS slices are in flight; every slice refills the slot that it frees (past
-  // the end with loads that nothing reads), so every wait counts alike.  The next
-  // step's operands are read behind the first instruction of a step, the next
-  // slice's behind the barrier in the last step.
+  // 16.  NS slices are in flight: the last step of a slice waits for the next one,
+  // passes the barrier behind which its own slot is free, and refills that slot (past
+  // the end with loads that nothing reads, so that every wait counts alike).
+  // The loads and the LDS reads of the next step's operands stand one by one between
+  // the matrix instructions: issued together behind the barrier, the loads, which
+  // enter the memory pipe one in 16 cycles, kept their waves and with them the
+  // matrix units waiting (8192 x 4096, k 14336: 428 against 412 us).
   __device__ static void run(const Q8Args& g, Smem& sm, int64_t m0, int64_t n0, int wave, int lane,
                              const Reads& rd, v16i (&acc)[IM][IN]) {
+    constexpr int MF = IM * IN, RD = IM + IN;
     const int K = static_cast<int>(g.k);
     const int nslices = (K + BK - 1) / BK, last = K - kChunk;
     const Src src = sources(g, m0, n0, wave, lane);
 #pragma unroll
-    for (int s = 0; s < NS; ++s) issue(sm, src, s, s, wave, last);
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+      for (int u = 0; u < PER; ++u) issue(sm, src, u, s, s, wave, last);
     wait_vmcnt<(NS - 1) * PER>();
     lds_barrier();
     Pack pk[2];
-    read_pack(sm.a[0], sm.b[0], rd, 0, pk[0]);
+#pragma unroll
+    for (int r = 0; r < RD; ++r) read_one(sm.a[0], sm.b[0], rd, 0, r, pk[0]);
     int slot = 0;
     for (int s = 0; s + 1 < nslices; ++s) {
-      const int nslot = slot + 1 == NS ? 0 : slot + 1;
+      const int next = slot + 1 == NS ? 0 : slot + 1;
 #pragma unroll
       for (int q = 0; q < STEPS; ++q) {
-        steps<0, 1>(pk[q & 1], acc);
-        __builtin_amdgcn_sched_barrier(0);
-        if (q + 1 < STEPS) {
-          read_pack(sm.a[slot], sm.b[slot], rd, q + 1, pk[(q + 1) & 1]);
-        } else {
-          wait_vmcnt<(NS - 2) * PER>();
-          lds_barrier();
-          issue(sm, src, s + NS, slot, wave, last);
-          read_pack(sm.a[nslot], sm.b[nslot], rd, 0, pk[0]);
+        const bool closing = q + 1 == STEPS;
+#pragma unroll
+        for (int t = 0; t < MF; ++t) {
+          step(pk[q & 1], t, acc);
+          __builtin_amdgcn_sched_barrier(0);
+          if (closing && t == 0) {
+            wait_vmcnt<(NS - 2) * PER>();
+            lds_barrier();
+          }
+#pragma unroll
+          for (int r = RD * t / MF; r < RD * (t + 1) / MF; ++r)
+            read_one(sm.a[closing ? next : slot], sm.b[closing ? next : slot], rd,
+                     closing ? 0 : q + 1, r, pk[(q + 1) & 1]);
+          if (closing) {
+#pragma unroll
+            for (int u = PER * t / MF; u < PER * (t + 1) / MF; ++u)
+              issue(sm, src, u, s + NS, slot, wave, last);
+          }
+          __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
-        steps<1, IM * IN>(pk[q & 1], acc);
-        __builtin_amdgcn_sched_barrier(0);
       }
-      slot = nslot;
+      slot = next;
     }
     // the last slice, cut by K
 #pragma unroll
     for (int q = 0; q < STEPS; ++q) {
-      if (q + 1 < STEPS) read_pack(sm.a[slot], sm.b[slot], rd, q + 1, pk[(q + 1) & 1]);
+      if (q + 1 < STEPS) {
+#pragma unroll
+        for (int r = 0; r < RD; ++r)
+          read_one(sm.a[slot], sm.b[slot], rd, q + 1, r, pk[(q + 1) & 1]);
+      }
       const int kk = (nslices - 1) * BK + (2 * q + (lane >> 5)) * kChunk;
       if (kk >= K) {
 #pragma unroll
         for (int i = 0; i < IM; ++i) pk[q & 1].a[i] = v4i{0, 0, 0, 0};
       }
-      steps<0, IM * IN>(pk[q & 1], acc);
+#pragma unroll
+      for (int t = 0; t < MF; ++t) step(pk[q & 1], t, acc);
     }
-    wait_vmcnt<0>();  // no load may reach LDS behind this workgroup
+    wait_vmcnt<0>();  // no load may reach LDS from here on
+    __syncthreads();
   }
 
   // Any alignment and any K: slices through registers into a pair of slots.
@@ -248,47 +263,71 @@ struct Q8Tile {
 #pragma unroll
       for (int q = 0; q < STEPS; ++q) {
         Pack pk;
-        read_pack(sm.a[slot], sm.b[slot], rd, q, pk);
-        steps<0, IM * IN>(pk, acc);
+#pragma unroll
+        for (int r = 0; r < IM + IN; ++r) read_one(sm.a[slot], sm.b[slot], rd, q, r, pk);
+#pragma unroll
+        for (int t = 0; t < IM * IN; ++t) step(pk, t, acc);
       }
       if (s + 1 < nslices) put(slot ^ 1);  // its last readers are behind the barrier below
       __syncthreads();
     }
   }
 
-  // Instruction tile element r of a lane: row 8 (r / 4) + 4 (lane / 32) + r % 4,
-  // column lane % 32.
+  // Instruction tile element r of a lane is row 8 (r / 4) + 4 (lane / 32) + r % 4,
+  // column lane % 32: stored from there, a wave's store would hold 4 bytes a lane.
+  // Each wave turns 32 of its rows at a time in its own part of LDS (free by now)
+  // into 4 columns a lane and stores 16 bytes.  A pitch of 8 more than a multiple of
+  // 16 words puts the two half-waves' rows (4 apart) into different banks.
   // INNER: the wave's outputs all lie inside C.
   template <bool INNER>
-  __device__ static void store(const Q8Args& g, int64_t m0, int64_t n0, int lane,
-                               const v16i (&acc)[IM][IN]) {
-    const int64_t col = n0 + (lane & 31);
-    float sb[IN], bias[IN];
+  __device__ static void store(const Q8Args& g, Smem& sm, int64_t m0, int64_t n0, int wave,
+                               int lane, const v16i (&acc)[IM][IN]) {
+    constexpr int LPR = TN / 4, RPS = 64 / LPR;  // lanes per row, rows per store
+    int* turn = sm.turn[wave];
+    const int64_t col = n0 + lane % LPR * 4;
+    float sb[4], bias[4];
 #pragma unroll
-    for (int j = 0; j < IN; ++j) {
-      const bool in = INNER || col + 32 * j < g.n;
-      sb[j] = in ? g.b_scale[col + 32 * j] : 0.0f;
-      bias[j] = in && g.bias ? g.bias[col + 32 * j] : 0.0f;
+    for (int c = 0; c < 4; ++c) {
+      const bool in = INNER || col + c < g.n;
+      sb[c] = in ? g.b_scale[col + c] : 0.0f;
+      bias[c] = in && g.bias ? g.bias[col + c] : 0.0f;
     }
 #pragma unroll
     for (int i = 0; i < IM; ++i) {
-      const int64_t row0 = m0 + 32 * i + 4 * (lane >> 5);
-      float sa[16];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int64_t row = row0 + 8 * (r / 4) + r % 4;
-        sa[r] = INNER || row < g.m ? g.a_scale[row] : 0.0f;
-      }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int64_t row = row0 + 8 * (r / 4) + r % 4;
-        float* c = g.C + row * g.ldc + col;
+      for (int r = 0; r < 16; ++r)
 #pragma unroll
         for (int j = 0; j < IN; ++j)
-          if (INNER || (row < g.m && col + 32 * j < g.n)) {
-            const float v = q8_output(acc[i][j][r], sa[r], sb[j]);
-            c[32 * j] = g.bias ? v + bias[j] : v;
+          turn[(8 * (r / 4) + 4 * (lane >> 5) + r % 4) * PITCH + 32 * j + (lane & 31)] =
+              acc[i][j][r];
+      // (one wave's LDS operations complete in order)
+#pragma unroll
+      for (int t = 0; t < 32 / RPS; ++t) {
+        const int r = t * RPS + lane / LPR;
+        const int64_t row = m0 + 32 * i + r;
+        const v4i sum = *reinterpret_cast<const v4i*>(turn + r * PITCH + lane % LPR * 4);
+        if (!INNER && row >= g.m) continue;
+        const float sa = g.a_scale[row];
+        float v[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          v[c] = q8_output(sum[c], sa, sb[c]);
+          if (g.bias) v[c] = v[c] + bias[c];
+        }
+        float* out = g.C + row * g.ldc + col;
+        if (INNER || col + 4 <= g.n) {
+          if constexpr (BM == 256) {
+            // a large product's output goes past the caches, which hold its operands
+            typedef float v4f __attribute__((ext_vector_type(4), aligned(4)));
+            __builtin_nontemporal_store(v4f{v[0], v[1], v[2], v[3]}, reinterpret_cast<v4f*>(out));
+          } else {
+            __builtin_memcpy(out, v, sizeof(v));
           }
+        } else {
+#pragma unroll
+          for (int c = 0; c < 3; ++c)
+            if (col + c < g.n) out[c] = v[c];
+        }
       }
     }
   }
@@ -297,7 +336,7 @@ struct Q8Tile {
 // Workgroups are dealt to the 8 XCDs in turn; each XCD takes a stretch of the
 // tiles, which go down columns of kGroup tile rows, so that the tiles it runs at
 // one time share their panels in its L2.
-constexpr int kGroup = 4;
+constexpr int kGroup = 8;
 __device__ __forceinline__ bool locate(int64_t tiles_m, int64_t tiles_n, int64_t per, int64_t* tm,
                                        int64_t* tn) {
   const int64_t t = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
@@ -330,15 +369,16 @@ __global__ __launch_bounds__(WM* WN * 64) void q8_tile_kernel(Q8Args g, int64_t 
   else Tile::run(g, sm, tm * BM, tn * BN, wave, lane, rd, acc);
   const int64_t m0 = tm * BM + wm0, n0 = tn * BN + wn0;
   if (m0 + Tile::TM <= g.m && n0 + Tile::TN <= g.n)
-    Tile::template store<true>(g, m0, n0, lane, acc);
+    Tile::template store<true>(g, sm, m0, n0, wave, lane, acc);
   else
-    Tile::template store<false>(g, m0, n0, lane, acc);
+    Tile::template store<false>(g, sm, m0, n0, wave, lane, acc);
 }
 
 // ---------------------------------------------------------------------------
 // Few rows: bound by reading B.  A workgroup owns 16 columns and MT tiles of 16
-// rows; its waves share the contraction, 64 codes each in turn, and the sums meet
-// in LDS.  Operands go from global memory to registers.
+// rows; its waves share the contraction, 128 codes each in turn (a whole line of
+// every row), and the sums meet in LDS.  Operands go from global
+// memory to registers; the lanes of rows past the last one load nothing.
 // ---------------------------------------------------------------------------
 
 constexpr int kFewWaves = 8;
@@ -349,51 +389,71 @@ __global__ __launch_bounds__(kFewWaves * 64) void q8_few_kernel(Q8Args g) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r16 = lane & 15, quarter = lane >> 4;
+  const int64_t K = g.k;
+  const int8_t* a[MT];
+  bool live[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    live[t] = t * 16 + r16 < g.m;
+    a[t] = g.A + (live[t] ? t * 16 + r16 : 0) * g.lda + quarter * 32;
+  }
   for (int64_t n0 = static_cast<int64_t>(blockIdx.x) * 16; n0 < g.n;
        n0 += static_cast<int64_t>(gridDim.x) * 16) {
-    const int64_t j = n0 + r16 < g.n ? n0 + r16 : g.n - 1;
-    const int8_t* b = g.B + j * g.ldb;
-    const int8_t* a[MT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) {
-      const int64_t i = t * 16 + r16 < g.m ? t * 16 + r16 : g.m - 1;
-      a[t] = g.A + i * g.lda;
-    }
+    const int64_t j = n0 + r16;
+    const int8_t* b = g.B + (j < g.n ? j : g.n - 1) * g.ldb + quarter * 32;
     v4i acc[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t) acc[t] = v4i{0, 0, 0, 0};
-    const int64_t K = g.k;
-    constexpr int U = MT == 1 ? 8 : 4;  // steps in flight
-    const int64_t step = kFewWaves * 64;
-    int64_t k0 = wave * 64;
-    for (; k0 + (U - 1) * step + 64 <= K; k0 += U * step) {
-      v4i bv[U], av[U][MT];
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        __builtin_memcpy(&bv[u], b + k0 + u * step + quarter * kChunk, kChunk);
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int t = 0; t < MT; ++t)
-          __builtin_memcpy(&av[u][t], a[t] + k0 + u * step + quarter * kChunk, kChunk);
+    // A step is 128 codes: a lane's 32 of them feed two instructions.  (Which k an
+    // operand's place stands for is free as long as A's and B's agree.)
+    constexpr int U = 4;  // steps in flight
+    constexpr int64_t kStep = kFewWaves * 128;
+    int64_t k0 = wave * 128;
+    for (; k0 + (U - 1) * kStep + 128 <= K; k0 += U * kStep) {
+      v4i bv[U][2], av[U][2][MT];
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
-          acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(av[u][t], bv[u], acc[t], 0, 0, 0);
+        for (int h = 0; h < 2; ++h)
+          __builtin_memcpy(&bv[u][h], b + k0 + u * kStep + h * kChunk, kChunk);
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) av[u][h][t] = v4i{0, 0, 0, 0};
+        if (live[t]) {
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              __builtin_memcpy(&av[u][h][t], a[t] + k0 + u * kStep + h * kChunk, kChunk);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int t = 0; t < MT; ++t)
+            acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(av[u][h][t], bv[u][h], acc[t], 0, 0, 0);
     }
-    for (; k0 < K; k0 += step) {
-      const v4i bv = load_codes(b, k0 + quarter * kChunk, K);
+    for (; k0 < K; k0 += kStep) {
 #pragma unroll
-      for (int t = 0; t < MT; ++t)
-        acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(load_codes(a[t], k0 + quarter * kChunk, K), bv,
-                                                       acc[t], 0, 0, 0);
+      for (int h = 0; h < 2; ++h) {
+        const int64_t kk = k0 + h * kChunk, end = K - quarter * 32;
+        const v4i bv = load_codes(b, kk, end);
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+          acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(
+              live[t] ? load_codes(a[t], kk, end) : v4i{0, 0, 0, 0}, bv, acc[t], 0, 0, 0);
+      }
     }
     // element r of a lane: row 4 (lane / 16) + r, column lane % 16
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) part[wave][t * 256 + (quarter * 4 + r) * 16 + r16] = acc[t][r];
+      for (int r = 0; r < 4; ++r) part[wave][(t * 16 + quarter * 4 + r) * 16 + r16] = acc[t][r];
     __syncthreads();
     for (int o = threadIdx.x; o < MT * 256; o += kFewWaves * 64) {
       const int64_t row = o / 16, col = n0 + o % 16;
@@ -406,6 +466,14 @@ __global__ __launch_bounds__(kFewWaves * 64) void q8_few_kernel(Q8Args g) {
     }
     __syncthreads();  // the sums are read before the next columns'
   }
+}
+
+template <int MT>
+hipError_t launch_few(const Q8Args& g, hipStream_t s) {
+  const int64_t groups = (g.n + 16 - 1) / 16, cap = int64_t(1) << 22;
+  hipLaunchKernelGGL(q8_few_kernel<MT>, dim3(static_cast<unsigned>(groups < cap ? groups : cap)),
+                     dim3(kFewWaves * 64), 0, s, g);
+  return hipGetLastError();
 }
 
 template <int BM, int BN, int WM, int WN, int BK, int NS, bool ANY>
@@ -424,24 +492,30 @@ hipError_t launch_matmul_q8(const Q8Args& g, hipStream_t s) {
   const bool direct = g.k > 0 && g.k % kChunk == 0 && g.lda % kChunk == 0 && g.ldb % kChunk == 0 &&
                       reinterpret_cast<uintptr_t>(g.A) % kChunk == 0 &&
                       reinterpret_cast<uintptr_t>(g.B) % kChunk == 0;
-  if (g.m <= 64) {
-    const int64_t groups = (g.n + 15) / 16, cap = int64_t(1) << 22;
-    const dim3 grid(static_cast<unsigned>(groups < cap ? groups : cap)), block(kFewWaves * 64);
-    if (g.m <= 16) hipLaunchKernelGGL(q8_few_kernel<1>, grid, block, 0, s, g);
-    else if (g.m <= 32) hipLaunchKernelGGL(q8_few_kernel<2>, grid, block, 0, s, g);
-    else hipLaunchKernelGGL(q8_few_kernel<4>, grid, block, 0, s, g);
-    return hipGetLastError();
+  // Up to 8 rows, and up to 32 with few columns, where tiles are too few to read B
+  // with (4 x 32000, k 4096: 27.9 us against 31.2 with 64 x 64 tiles; 32 x 4096, k
+  // 14336: 25 against 32; but 32 x 14336, k 4096: 29 against 15.6, and 16 rows 18.2 against 15.2).
+  if (g.m <= 8) return launch_few<1>(g, s);
+  if (g.m <= 32 && g.n < 8192) return g.m <= 16 ? launch_few<1>(g, s) : launch_few<2>(g, s);
+  // Otherwise the tiles with the smallest estimate: rounds over the compute units
+  // times slices times what a slice of such a tile takes a compute unit, measured
+  // with 4096 and 14336 columns (225, 640 and 1970 ns; the larger a tile, the fewer of its operands are loaded twice).
+  // Up to one 128 x 128 tile a unit, a deeper ring of slices makes up for the
+  // second workgroup (256 x 14336, k 4096: 27 us against 35).
+  const int64_t cus = device_cus() > 0 ? device_cus() : 256;
+  auto tiles = [&](int64_t edge) { return ((g.m + edge - 1) / edge) * ((g.n + edge - 1) / edge); };
+  auto cost = [&](int64_t edge, int64_t ns) { return (tiles(edge) + cus - 1) / cus * ns; };
+  const int64_t small = cost(64, 225), middle = cost(128, 640), large = cost(256, 1970);
+  if (large <= middle && large <= small)
+    return direct ? launch_tiles<256, 256, 2, 4, 128, 2, false>(g, s)
+                  : launch_tiles<256, 256, 2, 4, 128, 2, true>(g, s);
+  if (middle < small) {
+    if (!direct) return launch_tiles<128, 128, 2, 4, 128, 2, true>(g, s);
+    return tiles(128) <= cus ? launch_tiles<128, 128, 2, 4, 128, 4, false>(g, s)
+                             : launch_tiles<128, 128, 2, 2, 128, 2, false>(g, s);
   }
-  const int64_t large = ((g.m + 255) / 256) * ((g.n + 255) / 256);
-  const int64_t middle = ((g.m + 127) / 128) * ((g.n + 127) / 128);
-  if (large >= 192)
-    return direct ? launch_tiles<256, 256, 2, 4, 64, 4, false>(g, s)
-                  : launch_tiles<256, 256, 2, 4, 64, 2, true>(g, s);
-  if (middle >= 192)
-    return direct ? launch_tiles<128, 128, 2, 2, 64, 4, false>(g, s)
-                  : launch_tiles<128, 128, 2, 2, 64, 2, true>(g, s);
-  return direct ? launch_tiles<64, 64, 2, 2, 64, 4, false>(g, s)
-                : launch_tiles<64, 64, 2, 2, 64, 2, true>(g, s);
+  return direct ? launch_tiles<64, 64, 2, 2, 128, 4, false>(g, s)
+                : launch_tiles<64, 64, 2, 2, 128, 2, true>(g, s);
 }
 
 }  // namespace repops
