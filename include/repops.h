@@ -751,8 +751,10 @@ repops_status_t repops_sample_workspace(int64_t rows, int64_t vocab, uint64_t *b
  * but its inputs.  With m the row's largest logit:
  *     it = 1 / temperature;  d_j = (l_j - m) * it in binary64 (0 where l_j = m);
  *     w_j = rint(exp(d_j) * 2^43), an integer: 0 for d_j <= -31, else
- *         n = rint(d * log2(e));  r = fma(n, -ln2_hi, d);  r = fma(n, -ln2_lo, r);
- *         p = Horner over 1/i!, i = 11..0, with fma;  w = rint(p * 2^(n + 43)).
+ *         b = rint(-64 d);  r = fma(b, 1/64, d);
+ *         p = Horner over 1/i!, i = 5..0, with fma;  w = rint(e(-b/64) * p), rounded once;
+ *         e(x):  n = rint(x * log2(e));  r = fma(n, -ln2_hi, x);  r = fma(n, -ln2_lo, r);
+ *         q = Horner over 1/i!, i = 11..0, with fma;  e = q * 2^(n + 43).
  *   The tokens are taken in order of descending logit, equal ones by ascending
  *   index (-0 and +0 are equal).  Each filter keeps a prefix of that order, the
  *   first token always; the shortest prefix holds:

@@ -20,10 +20,9 @@ static int by_logit(const void *pa, const void *pb)
     return a->j < b->j ? -1 : a->j > b->j;
 }
 
-/* w = rint(exp(d) 2^43) by the stated sequence; 0 for d <= -31 or NaN. */
-uint64_t sample_ref_weight(double d)
+/* exp(d) 2^43 for d in [-31, 0], by the stated sequence. */
+static double exp43(double d)
 {
-    if (!(d > -31.0)) return 0;
     const double n = rint(d * 1.4426950408889634);
     const double ln2_hi = 0x1.62e42fefa3p-1, ln2_lo = 0x1.3de6af278ece6p-42;
     double r = fma(n, -ln2_hi, d);
@@ -33,7 +32,20 @@ uint64_t sample_ref_weight(double d)
         fact = fact / (double)(i + 1);
         p = fma(p, r, 1.0 / fact);
     }
-    return (uint64_t)rint(ldexp(p, (int)n + 43));
+    return ldexp(p, (int)n + 43);
+}
+
+/* w = rint(exp(d) 2^43): exp(-b/64) exp(d + b/64); 0 for d <= -31 or NaN. */
+uint64_t sample_ref_weight(double d)
+{
+    if (!(d > -31.0)) return 0;
+    const double b = rint(d * -64.0);
+    const double r = fma(b, 1.0 / 64.0, d);
+    const double f[6] = {1.0, 1.0, 1.0 / 2.0, 1.0 / 6.0, 1.0 / 24.0, 1.0 / 120.0};
+    double p = f[5];
+    for (int i = 4; i >= 0; --i) p = fma(p, r, f[i]);
+    /* one rounding of the product to an integer */
+    return (uint64_t)(fma(exp43(b * (-1.0 / 64.0)), p, 0x1p52) - 0x1p52);
 }
 
 double sample_ref_log(float m)

@@ -3,11 +3,17 @@
 // Weights are integers, w = rint(exp((l - max) / T) 2^43): their sums are exact
 // in 64 bits in any order (at most 2^20 tokens), so no reduction's shape can
 // change a token.  Nothing is sorted as a whole.  The row's tokens go into
-// buckets by (max - l) / T, 64 to a unit; the running weight (or count) over the
-// buckets finds the one that holds a filter's end or the draw, and only that
+// buckets by d = (l - max) / T, 64 to a unit; the running weight (or count) over
+// the buckets finds the one that holds a filter's end or the draw, and only that
 // bucket's tokens are put in order, each one's place found by comparing it with
-// the others.  A bucket too full for that (many equal logits, or a
-// high temperature) is narrowed by its keys first.
+// the others.  A bucket too full for that (many equal logits, or a high
+// temperature) is narrowed by its keys first.
+//
+// The bucket also carries the exponential: with b = rint(-64 d) and r = d + b/64,
+// exp(d) = exp(-b/64) exp(r), |r| <= 1/128, so a table of the first factor (built
+// with the full polynomial) leaves five fused steps per token.  A row is read for
+// its maximum, for the buckets' weights, and for the tokens of the buckets wanted;
+// up to 32768 tokens stay in registers between.
 #include <hip/hip_runtime.h>
 
 #include "generation_internal.h"
@@ -19,19 +25,22 @@ namespace {
 
 constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
-constexpr double kSpan = 31.0;               // exp(-31) < 2^-44: a weight of 0
-constexpr int kPerUnit = 64;                 // buckets per unit of d
-constexpr int kBuckets = 31 * kPerUnit + 1;  // the last: weight 0
-constexpr int kList = 2048;                  // tokens put in order at once
+constexpr double kSpan = 31.0;        // exp(-31) < 2^-44: a weight of 0
+constexpr int kPerUnit = 64;          // buckets per unit of d
+constexpr int kWeighted = 31 * kPerUnit + 1;  // buckets 0 .. 1984: rint(64 * 31)
+constexpr int kBuckets = kWeighted + 1;       // the last one: weight 0
+constexpr int kList = 2048;           // tokens collected at once
+constexpr int kSmall = kThreads;      // tokens put in order at once
+constexpr int kSub = 1024;            // parts that a bucket's keys are narrowed by
 
-// rint(exp(d) 2^43), d in (-31, 0].  The degree-11 Taylor polynomial is within
-// 7e-15 of exp, a ninth of half a unit at the largest weight.
-__device__ __forceinline__ uint64_t weight_of(double d) {
+// exp(d) 2^43 for d in [-31, 0]: the degree-11 Taylor polynomial is within 7e-15
+// of exp.
+__device__ __forceinline__ double exp43(double d) {
   const double n = __builtin_rint(d * 1.4426950408889634);
   // ln2 as its first 41 bits (n times them is exact) and the rest
   double r = __builtin_fma(n, -0x1.62e42fefa3000p-1, d);
   r = __builtin_fma(n, -0x1.3de6af278ece6p-42, r);
-  double p = 0x1.ae64567f544e4p-26;              // 1/11!
+  double p = 0x1.ae64567f544e4p-26;                // 1/11!
   p = __builtin_fma(p, r, 0x1.27e4fb7789f5cp-22);  // 1/10!
   p = __builtin_fma(p, r, 0x1.71de3a556c734p-19);
   p = __builtin_fma(p, r, 0x1.a01a01a01a01ap-16);
@@ -43,16 +52,12 @@ __device__ __forceinline__ uint64_t weight_of(double d) {
   p = __builtin_fma(p, r, 0.5);
   p = __builtin_fma(p, r, 1.0);
   p = __builtin_fma(p, r, 1.0);
-  // p 2^(43 + n) is exact; adding 2^52 rounds it to an integer (ties to even)
-  const double scale =
-      __hiloint2double((1023 + 43 + static_cast<int>(n)) << 20, 0);
-  const double t = __builtin_fma(p, scale, 0x1p52);
-  return static_cast<uint64_t>(__double_as_longlong(t)) & 0xfffffffffffffull;
+  return p * __hiloint2double((1023 + 43 + static_cast<int>(n)) << 20, 0);  // exact
 }
 
 // Natural logarithm of m in (0, 1).
 __device__ double log_of(float m) {
-  uint64_t b = static_cast<uint64_t>(__double_as_longlong(static_cast<double>(m)));
+  const uint64_t b = static_cast<uint64_t>(__double_as_longlong(static_cast<double>(m)));
   int e = static_cast<int>(b >> 52) - 1023;
   double f = __longlong_as_double(static_cast<int64_t>((b & 0xfffffffffffffull) | (1023ull << 52)));
   if (f > 0x1.6a09e667f3bcdp+0) {
@@ -75,37 +80,130 @@ __device__ double log_of(float m) {
   return __builtin_fma(static_cast<double>(e), 0x1.62e42fefa39efp-1, two_s * p);
 }
 
-// Larger logits have larger keys; -0 and +0 share one.
+// Larger logits have larger keys; -0 and +0 share one.  A NaN's is the largest.
+constexpr uint32_t kNanKey = 0xffffffffu;
 __device__ __forceinline__ uint32_t key_of(float l) {
   uint32_t b = __float_as_uint(l);
   if (b == 0x80000000u) b = 0;
-  return (b & 0x80000000u) ? ~b : b | 0x80000000u;
+  b = (b & 0x80000000u) ? ~b : b | 0x80000000u;
+  return l != l ? kNanKey : b;
+}
+__device__ __forceinline__ float logit_of(uint32_t key) {
+  return __uint_as_float((key & 0x80000000u) ? key & 0x7fffffffu : ~key);
 }
 
+struct Shared {
+  uint64_t before[kBuckets + 1];  // weights per bucket, then the running weight before each
+  uint32_t places[kBuckets + 1];  // counts likewise
+  double table[kWeighted];        // exp(-b / 64) 2^43
+  union {
+    struct {
+      uint64_t list[kList];       // (key, ~index): larger comes first in the order
+      uint64_t small[kSmall];
+      uint64_t small_w[kSmall];
+    };
+    struct {
+      uint64_t sub_w[kSub];
+      uint32_t sub_c[kSub];
+    };
+  };
+  uint64_t wave_w[kWaves];
+  uint32_t wave_c[kWaves];
+  uint64_t found_before, found_w;
+  uint32_t found_index, n_list, n_small, lo, hi;
+  int found_bucket;
+};
+
+// Where a logit stands: d, its bucket and, asked for, its weight.
 struct Scale {
   float top;       // the row's largest logit
   double inverse;  // 1 / temperature
   __device__ __forceinline__ double d(float l) const {
-    return l == top ? 0.0 : (static_cast<double>(l) - static_cast<double>(top)) * inverse;
+    const double v = (static_cast<double>(l) - static_cast<double>(top)) * inverse;
+    return l == top ? 0.0 : v;  // (also where both are infinite)
+  }
+  // 2^52 + rint(-64 d): the bucket in its low word
+  static __device__ __forceinline__ double shifted(double d) {
+    return __builtin_fma(d, -static_cast<double>(kPerUnit), 0x1p52);
+  }
+  static __device__ __forceinline__ bool weighs(double d) { return d > -kSpan; }  // no NaN either
+  __device__ __forceinline__ int bucket(float l) const {
+    const double v = d(l);
+    return weighs(v) ? __double2loint(shifted(v)) : kBuckets - 1;
+  }
+  // for d that weighs
+  static __device__ __forceinline__ uint64_t weight(const double* table, double d, int* bucket) {
+    const double t = shifted(d);
+    *bucket = __double2loint(t);
+    const double r = __builtin_fma(t - 0x1p52, 1.0 / kPerUnit, d);
+    double p = 0x1.1111111111111p-7;  // 1/5!
+    p = __builtin_fma(p, r, 0x1.5555555555555p-5);
+    p = __builtin_fma(p, r, 0x1.5555555555555p-3);
+    p = __builtin_fma(p, r, 0.5);
+    p = __builtin_fma(p, r, 1.0);
+    p = __builtin_fma(p, r, 1.0);
+    // adding 2^52 rounds to an integer (ties to even)
+    const double w = __builtin_fma(table[*bucket], p, 0x1p52);
+    return static_cast<uint64_t>(__double_as_longlong(w)) & 0xfffffffffffffull;
+  }
+  __device__ __forceinline__ uint64_t weight(const double* table, float l) const {
+    const double v = d(l);
+    int b;
+    return weighs(v) ? weight(table, v, &b) : 0;
   }
 };
 
-// d is not below the span (a NaN, from infinities, is not either): a weight.
-__device__ __forceinline__ bool in_span(double d) { return d > -kSpan; }
-__device__ __forceinline__ int bucket_of(double d) {
-  return in_span(d) ? static_cast<int>(-d * kPerUnit) : kBuckets - 1;
-}
+// ---------------------------------------------------------------------------
+// A workgroup's view of a row: f(logit, index) for every token, in registers or
+// read again each time.
+// ---------------------------------------------------------------------------
 
-struct Shared {
-  uint64_t weight[kBuckets];
-  uint32_t count[kBuckets];
-  uint64_t list[kList];     // (key, ~index): the order's places, largest first
-  uint64_t list_w[kList];
-  uint64_t wave_w[kWaves];
-  uint32_t wave_c[kWaves];
-  uint64_t found_before, found_w;
-  uint32_t found_index, n_list, lo, hi;
-  int found_bucket;
+template <int PER>
+struct Held {
+  float v[PER];
+  int n;
+  __device__ __forceinline__ Held(const float* l, int n_) : n(n_) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int j = static_cast<int>(threadIdx.x) + i * kThreads;
+      v[i] = 0.0f;
+      if (j < n) v[i] = l[j];
+    }
+  }
+  template <class F>
+  __device__ __forceinline__ void each(F f) const {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int j = static_cast<int>(threadIdx.x) + i * kThreads;
+      if (j < n) f(v[i], j);
+    }
+  }
+};
+
+struct Streamed {
+  const float* l;
+  int n;
+  __device__ __forceinline__ Streamed(const float* l_, int n_) : l(l_), n(n_) {}
+  template <class F>
+  __device__ __forceinline__ void each(F f) const {
+    constexpr int U = 4;  // 16-byte loads in flight (any 4-byte alignment)
+    int j = static_cast<int>(threadIdx.x) * 4;
+    for (; j + (U - 1) * kThreads * 4 + 4 <= n; j += U * kThreads * 4) {
+      float4 x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) __builtin_memcpy(&x[u], l + j + u * kThreads * 4, 16);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int k = j + u * kThreads * 4;
+        f(x[u].x, k);
+        f(x[u].y, k + 1);
+        f(x[u].z, k + 2);
+        f(x[u].w, k + 3);
+      }
+    }
+    for (; j < n; j += kThreads * 4)
+      for (int k = j; k < j + 4 && k < n; ++k) f(l[k], k);
+  }
 };
 
 template <class T, class Op>
@@ -119,261 +217,380 @@ __device__ T block_reduce(T v, T* per_wave, Op op) {
   return r;
 }
 
-// Which token of the order: the first at which the running weight exceeds
-// `at` (by_count 0), or the one in place `at` (by_count 1).
-struct Found {
-  uint64_t before, w;  // weight of the tokens before it, its own
-  uint32_t index;
-};
+__device__ __forceinline__ void add_u64(uint64_t* p, uint64_t v) {
+  atomicAdd(reinterpret_cast<unsigned long long*>(p), static_cast<unsigned long long>(v));
+}
 
-// Turns sh.weight / sh.count, filled per bucket (the order goes through them
-// upwards), into the bucket holding `at`, with the weight and count before it.
-__device__ int find_bucket(Shared& sh, int buckets, bool by_count, uint64_t at, uint64_t* before_w,
-                           uint64_t* before_c) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int b0 = tid * 2;
-  uint64_t w0 = 0, w1 = 0;
-  uint32_t c0 = 0, c1 = 0;
-  if (b0 < buckets) { w0 = sh.weight[b0]; c0 = sh.count[b0]; }
-  if (b0 + 1 < buckets) { w1 = sh.weight[b0 + 1]; c1 = sh.count[b0 + 1]; }
+// before[] and places[] of `buckets` parts (at most 2 a thread) become the running
+// sums before each part, the total in entry `buckets`.
+__device__ void running(Shared& sh, uint64_t* w, uint32_t* c, int buckets) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = tid * 2;
+  const uint64_t w0 = b < buckets ? w[b] : 0, w1 = b + 1 < buckets ? w[b + 1] : 0;
+  const uint32_t c0 = b < buckets ? c[b] : 0, c1 = b + 1 < buckets ? c[b + 1] : 0;
   uint64_t sw = w0 + w1;
   uint32_t sc = c0 + c1;
   for (int s = 1; s < 64; s <<= 1) {
     const uint64_t ow = __shfl_up(sw, s);
     const uint32_t oc = __shfl_up(sc, s);
-    if (lane >= s) { sw += ow; sc += oc; }
-  }
-  if (lane == 63) { sh.wave_w[wave] = sw; sh.wave_c[wave] = sc; }
-  if (tid == 0) sh.found_bucket = -1;
-  __syncthreads();
-  for (int k = 0; k < wave; ++k) { sw += sh.wave_w[k]; sc += sh.wave_c[k]; }
-  uint64_t bw = sw - w0 - w1;
-  uint64_t bc = sc - c0 - c1;
-  for (int h = 0; h < 2; ++h) {
-    const uint64_t w = h ? w1 : w0;
-    const uint32_t c = h ? c1 : c0;
-    const bool hit = by_count ? at >= bc && at < bc + c : at >= bw && at < bw + w;
-    if (hit) {
-      sh.found_bucket = b0 + h;
-      sh.found_before = bw;
-      sh.found_w = bc;
+    if (lane >= s) {
+      sw += ow;
+      sc += oc;
     }
-    bw += w;
-    bc += c;
   }
+  if (lane == 63) {
+    sh.wave_w[wave] = sw;
+    sh.wave_c[wave] = sc;
+  }
+  __syncthreads();
+  for (int k = 0; k < wave; ++k) {
+    sw += sh.wave_w[k];
+    sc += sh.wave_c[k];
+  }
+  if (b <= buckets) {
+    w[b] = sw - w0 - w1;
+    c[b] = sc - c0 - c1;
+  }
+  if (b + 1 <= buckets) {
+    w[b + 1] = sw - w1;
+    c[b + 1] = sc - c1;
+  }
+  __syncthreads();
+}
+
+// The part whose running sums hold `at`.
+__device__ int part_of(Shared& sh, const uint64_t* w, const uint32_t* c, int buckets, bool by_count,
+                       uint64_t at) {
+  for (int b = threadIdx.x; b < buckets; b += kThreads)
+    if (by_count ? at >= c[b] && at < c[b + 1] : at >= w[b] && at < w[b + 1]) sh.found_bucket = b;
   __syncthreads();
   const int b = sh.found_bucket;
-  *before_w = sh.found_before;
-  *before_c = sh.found_w;
   __syncthreads();
   return b;
 }
 
-// The token of a row at `at` in the order: in the bucket that holds it, among
-// the tokens whose keys lie in an interval narrowed until they fit the list or
-// are all equal.
-__device__ Found locate(Shared& sh, const float* l, int64_t n, const Scale& sc, bool by_count,
-                        uint64_t at) {
-  const int tid = threadIdx.x;
-  uint64_t before_w, before_c;
-  // per-bucket sums of the row
-  for (int b = tid; b < kBuckets; b += kThreads) { sh.weight[b] = 0; sh.count[b] = 0; }
-  __syncthreads();
-  for (int64_t j = tid; j < n; j += kThreads) {
-    const double d = sc.d(l[j]);
-    const int b = bucket_of(d);
-    atomicAdd(&sh.count[b], 1u);
-    if (in_span(d))
-      atomicAdd(reinterpret_cast<unsigned long long*>(&sh.weight[b]),
-                static_cast<unsigned long long>(weight_of(d)));
+// A token of the order: the weight before it, its own, its index.
+struct Found {
+  uint64_t before, w;
+  uint32_t index;
+};
+
+// Collected tokens: those of the buckets lo .. hi.
+struct Listed {
+  int lo, hi;
+  uint32_t n;
+};
+
+// The token at `at` (weight or place before it) among the sh.n_small tokens of
+// sh.small, which follow `before` weight and `place` tokens: every token's place
+// by comparison with the others.
+__device__ Found among_small(Shared& sh, const Scale& sc, bool by_count, uint64_t at,
+                             uint64_t before, uint64_t place) {
+  const uint32_t n = sh.n_small, i = threadIdx.x;
+  uint64_t mine = 0, w = 0;
+  if (i < n) {
+    mine = sh.small[i];
+    w = sc.weight(sh.table, logit_of(static_cast<uint32_t>(mine >> 32)));
+    sh.small_w[i] = w;
   }
   __syncthreads();
-  const int bucket = find_bucket(sh, kBuckets, by_count, at, &before_w, &before_c);
-  uint32_t held = sh.count[bucket];
-  // the bucket's keys
-  if (tid == 0) { sh.lo = 0xffffffffu; sh.hi = 0; }
-  __syncthreads();
-  for (int64_t j = tid; j < n; j += kThreads)
-    if (bucket_of(sc.d(l[j])) == bucket) {
-      const uint32_t k = key_of(l[j]);
-      atomicMin(&sh.lo, k);
-      atomicMax(&sh.hi, k);
-    }
-  __syncthreads();
-  uint32_t lo = sh.lo, hi = sh.hi;
-  __syncthreads();
-  while (held > kList && lo != hi) {
-    int shift = 0;
-    while (((hi - lo) >> shift) >= 1024u) ++shift;
-    for (int b = tid; b < 1024; b += kThreads) { sh.weight[b] = 0; sh.count[b] = 0; }
-    __syncthreads();
-    for (int64_t j = tid; j < n; j += kThreads) {
-      const uint32_t k = key_of(l[j]);
-      if (k >= lo && k <= hi) {
-        const int b = static_cast<int>((hi - k) >> shift);
-        const double d = sc.d(l[j]);
-        atomicAdd(&sh.count[b], 1u);
-        if (in_span(d))
-          atomicAdd(reinterpret_cast<unsigned long long*>(&sh.weight[b]),
-                    static_cast<unsigned long long>(weight_of(d)));
+  if (i < n) {
+    uint64_t bw = before, bc = place;
+    for (uint32_t o = 0; o < n; ++o)
+      if (sh.small[o] > mine) {
+        bw += sh.small_w[o];
+        ++bc;
       }
+    if (by_count ? bc == at : at >= bw && at < bw + w) {
+      sh.found_before = bw;
+      sh.found_w = w;
+      sh.found_index = 0xffffffffu - static_cast<uint32_t>(mine);
     }
-    __syncthreads();
-    uint64_t bw, bc;
-    const int b = find_bucket(sh, 1024, by_count, by_count ? at - before_c : at - before_w, &bw, &bc);
-    held = sh.count[b];
-    before_w += bw;
-    before_c += bc;
-    const uint32_t top = hi - (static_cast<uint32_t>(b) << shift);
-    const uint32_t width = (1u << shift) - 1u;
-    lo = top - lo < width ? lo : top - width;
-    hi = top;
-    __syncthreads();
   }
-  Found f;
-  if (held <= kList) {
-    if (tid == 0) sh.n_list = 0;
-    __syncthreads();
-    for (int64_t j = tid; j < n; j += kThreads) {
-      const uint32_t k = key_of(l[j]);
-      if (k >= lo && k <= hi) {
-        const uint32_t at_list = atomicAdd(&sh.n_list, 1u);
-        const double d = sc.d(l[j]);
-        sh.list[at_list] = static_cast<uint64_t>(k) << 32 | (0xffffffffu - static_cast<uint32_t>(j));
-        sh.list_w[at_list] = in_span(d) ? weight_of(d) : 0;
-      }
-    }
-    __syncthreads();
-    for (uint32_t i = tid; i < held; i += kThreads) {
-      const uint64_t mine = sh.list[i], w = sh.list_w[i];
-      uint64_t bw = before_w, bc = before_c;
-      for (uint32_t o = 0; o < held; ++o)
-        if (sh.list[o] > mine) { bw += sh.list_w[o]; ++bc; }
-      if (by_count ? bc == at : at >= bw && at < bw + w) {
-        sh.found_before = bw;
-        sh.found_w = w;
-        sh.found_index = 0xffffffffu - static_cast<uint32_t>(mine);
-      }
-    }
-    __syncthreads();
-    f = {sh.found_before, sh.found_w, sh.found_index};
-    __syncthreads();
-    return f;
-  }
-  // Equal logits, more than the list holds: the place among them by index.  Each
-  // thread counts a stretch of the row, and the one whose stretch holds the
-  // place walks it.
-  double d = 0.0;
-  {
-    const uint32_t bits = (lo & 0x80000000u) ? lo & 0x7fffffffu : ~lo;
-    d = sc.d(__uint_as_float(bits));
-  }
-  const uint64_t w = in_span(d) ? weight_of(d) : 0;
-  const uint64_t place = by_count ? at - before_c : (at - before_w) / w;
-  const int64_t stretch = (n + kThreads - 1) / kThreads;
-  const int64_t j0 = tid * stretch, j1 = j0 + stretch < n ? j0 + stretch : n;
-  uint32_t mine = 0;
-  for (int64_t j = j0; j < j1; ++j) mine += key_of(l[j]) == lo;
-  uint32_t upto = mine;
-  const int lane = tid & 63, wave = tid >> 6;
-  for (int s = 1; s < 64; s <<= 1) {
-    const uint32_t o = __shfl_up(upto, s);
-    if (lane >= s) upto += o;
-  }
-  if (lane == 63) sh.wave_c[wave] = upto;
   __syncthreads();
-  for (int k = 0; k < wave; ++k) upto += sh.wave_c[k];
-  uint64_t c = upto - mine;
-  if (place >= c && place < upto)
-    for (int64_t j = j0; j < j1; ++j)
-      if (key_of(l[j]) == lo && c++ == place) sh.found_index = static_cast<uint32_t>(j);
-  __syncthreads();
-  f = {before_w + place * w, w, sh.found_index};
+  const Found f = {sh.found_before, sh.found_w, sh.found_index};
   __syncthreads();
   return f;
 }
 
-__global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
-  __shared__ Shared sh;
+__device__ __forceinline__ uint64_t entry_of(uint32_t key, int j) {
+  return static_cast<uint64_t>(key) << 32 | (0xffffffffu - static_cast<uint32_t>(j));
+}
+
+// A bucket with more tokens than kSmall: its keys' interval is cut into kSub parts
+// again and again, until the part that holds `at` is small or a single key.
+template <class Row>
+__device__ Found among_many(Shared& sh, const Row& row, const Scale& sc, int bucket, bool by_count,
+                            uint64_t at, uint64_t before, uint64_t place) {
   const int tid = threadIdx.x;
-  const int64_t n = a.vocab;
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const float* l = a.L + row * a.ldl;
-    // the largest key and whether a NaN is there
-    uint32_t top = 0, nan = 0;
-    for (int64_t j = tid; j < n; j += kThreads) {
-      const float v = l[j];
-      if (v != v) nan = 1;
-      const uint32_t k = key_of(v);
-      top = k > top ? k : top;
+  if (tid == 0) {
+    sh.lo = 0xffffffffu;
+    sh.hi = 0;
+  }
+  __syncthreads();
+  uint32_t least = 0xffffffffu, most = 0;
+  row.each([&](float l, int) {
+    if (sc.bucket(l) == bucket) {
+      const uint32_t k = key_of(l);
+      least = k < least ? k : least;
+      most = k > most ? k : most;
     }
-    nan = block_reduce(nan, sh.wave_c, [](uint32_t x, uint32_t y) { return x | y; });
-    top = block_reduce(top, sh.wave_c, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
-    const uint32_t bits = (top & 0x80000000u) ? top & 0x7fffffffu : ~top;
-    const float m = __uint_as_float(bits);
-    const float T = a.temperature ? a.temperature[row] : 1.0f;
-    uint32_t index = 0;
-    float prob = 1.0f;
-    bool drawn = true;
-    if (nan || n == 0 || m == -__builtin_inff()) {
-      drawn = false;
-      prob = nan ? __uint_as_float(0x7fc00000u) : 0.0f;
-    } else if (!(T > 0.0f)) {
-      uint32_t first = 0xffffffffu;
-      for (int64_t j = tid; j < n; j += kThreads)
-        if (key_of(l[j]) == top) first = static_cast<uint32_t>(j) < first ? static_cast<uint32_t>(j) : first;
-      index = block_reduce(first, sh.wave_c, [](uint32_t x, uint32_t y) { return x < y ? x : y; });
-    } else {
-      const Scale sc = {m, 1.0 / static_cast<double>(T)};
-      const float mp = a.min_p ? a.min_p[row] : 0.0f;
-      const double cut = mp > 0.0f ? (mp >= 1.0f ? 0.0 : log_of(mp)) : -1e300;
-      // the weight of all tokens and of those within min_p
-      uint64_t all = 0, near = 0;
-      for (int64_t j = tid; j < n; j += kThreads) {
-        const double d = sc.d(l[j]);
-        if (in_span(d)) {
-          const uint64_t w = weight_of(d);
-          all += w;
-          if (d >= cut) near += w;
-        }
+  });
+  if (least <= most) {
+    atomicMin(&sh.lo, least);
+    atomicMax(&sh.hi, most);
+  }
+  __syncthreads();
+  uint32_t lo = sh.lo, hi = sh.hi, held = kSmall + 1;
+  while (held > kSmall && lo != hi) {
+    int shift = 0;
+    while (((hi - lo) >> shift) >= kSub) ++shift;
+    __syncthreads();
+    sh.sub_w[tid] = 0;
+    sh.sub_c[tid] = 0;
+    __syncthreads();
+    row.each([&](float l, int) {
+      const uint32_t k = key_of(l);
+      if (k >= lo && k <= hi) {
+        const uint32_t b = (hi - k) >> shift;
+        atomicAdd(&sh.sub_c[b], 1u);
+        add_u64(&sh.sub_w[b], sc.weight(sh.table, l));
       }
-      auto add = [](uint64_t x, uint64_t y) { return x + y; };
-      uint64_t kept = block_reduce(all, sh.wave_w, add);
-      near = block_reduce(near, sh.wave_w, add);
-      const int64_t K = a.top_k ? a.top_k[row] : 0;
-      if (K > 0 && K < n) {
-        const Found f = locate(sh, l, n, sc, true, static_cast<uint64_t>(K - 1));
-        kept = f.before + f.w;
+    });
+    __syncthreads();
+    // the part that holds `at`, one thread a part
+    uint64_t bw = sh.sub_w[tid];
+    uint32_t bc = sh.sub_c[tid];
+    const uint64_t w = bw;
+    const uint32_t c = bc;
+    for (int s = 1; s < 64; s <<= 1) {
+      const uint64_t ow = __shfl_up(bw, s);
+      const uint32_t oc = __shfl_up(bc, s);
+      if ((tid & 63) >= s) {
+        bw += ow;
+        bc += oc;
       }
-      const float P = a.top_p ? a.top_p[row] : 1.0f;
-      if (P < 1.0f) {
-        uint64_t limit = 1;
-        if (P > 0.0f) {
-          const double x = __builtin_ceil(static_cast<double>(P) * static_cast<double>(kept));
-          limit = x < 1.0 ? 1 : static_cast<uint64_t>(x);
-          limit = limit < kept ? limit : kept;
-        }
-        const Found f = locate(sh, l, n, sc, false, limit - 1);
-        kept = f.before + f.w;
-      }
-      kept = near < kept ? near : kept;
-      const float u = a.u[row];
-      uint64_t at = 0;
-      if (u > 0.0f) {
-        if (u >= 1.0f) at = kept - 1;
-        else at = static_cast<uint64_t>(static_cast<double>(u) * static_cast<double>(kept));
-        at = at < kept - 1 ? at : kept - 1;
-      }
-      const Found f = locate(sh, l, n, sc, false, at);
-      index = f.index;
-      prob = static_cast<float>(static_cast<double>(f.w) / static_cast<double>(kept));
     }
-    if (tid == 0) {
-      a.token[row] = drawn ? static_cast<int32_t>(index) : -1;
-      if (a.prob) a.prob[row] = prob;
+    if ((tid & 63) == 63) {
+      sh.wave_w[tid >> 6] = bw;
+      sh.wave_c[tid >> 6] = bc;
     }
     __syncthreads();
+    for (int k = 0; k < tid >> 6; ++k) {
+      bw += sh.wave_w[k];
+      bc += sh.wave_c[k];
+    }
+    bw = bw - w + before;
+    const uint64_t bp = bc - c + place;
+    if (by_count ? at >= bp && at < bp + c : at >= bw && at < bw + w) {
+      sh.found_bucket = tid;
+      sh.found_before = bw;
+      sh.found_w = bp;
+      sh.n_small = c;
+    }
+    __syncthreads();
+    before = sh.found_before;
+    place = sh.found_w;
+    held = sh.n_small;
+    hi = hi - (static_cast<uint32_t>(sh.found_bucket) << shift);
+    const uint32_t width = (1u << shift) - 1u;
+    lo = hi - lo < width ? lo : hi - width;
+    __syncthreads();
   }
+  if (held <= kSmall) {
+    __syncthreads();
+    if (tid == 0) sh.n_small = 0;
+    __syncthreads();
+    row.each([&](float l, int j) {
+      const uint32_t k = key_of(l);
+      if (k >= lo && k <= hi) sh.small[atomicAdd(&sh.n_small, 1u)] = entry_of(k, j);
+    });
+    __syncthreads();
+    return among_small(sh, sc, by_count, at, before, place);
+  }
+  // Equal logits, as many as there are: the place among them in order of the index.
+  // The indices are cut into kSub parts in the same way.
+  const uint64_t w = sc.weight(sh.table, logit_of(lo));
+  const uint64_t want = by_count ? at - place : (at - before) / w;
+  uint32_t first = 0, span = static_cast<uint32_t>(row.n);
+  uint64_t skipped = 0;
+  while (span > 1) {
+    const uint32_t part = (span + kSub - 1) / kSub;
+    __syncthreads();
+    sh.sub_c[tid] = 0;
+    __syncthreads();
+    row.each([&](float l, int j) {
+      const uint32_t at_j = static_cast<uint32_t>(j) - first;
+      if (at_j < span && key_of(l) == lo) atomicAdd(&sh.sub_c[at_j / part], 1u);
+    });
+    __syncthreads();
+    uint32_t c = sh.sub_c[tid], upto = c;
+    for (int s = 1; s < 64; s <<= 1) {
+      const uint32_t o = __shfl_up(upto, s);
+      if ((tid & 63) >= s) upto += o;
+    }
+    if ((tid & 63) == 63) sh.wave_c[tid >> 6] = upto;
+    __syncthreads();
+    for (int k = 0; k < tid >> 6; ++k) upto += sh.wave_c[k];
+    const uint64_t b = skipped + upto - c;
+    if (want >= b && want < b + c) {
+      sh.found_bucket = tid;
+      sh.found_w = b;
+    }
+    __syncthreads();
+    first += static_cast<uint32_t>(sh.found_bucket) * part;
+    skipped = sh.found_w;
+    span = part;
+    __syncthreads();
+  }
+  return {before + want * w, w, first};
+}
+
+// The token at `at` of the order: the first at which the running weight exceeds
+// `at`, or (by_count) the one in that place.  `reach`: also collect the buckets
+// before it, if they fit, for the searches that follow.
+template <class Row>
+__device__ Found locate(Shared& sh, const Row& row, const Scale& sc, bool by_count, uint64_t at,
+                        bool counted, bool reach, Listed& listed) {
+  const int tid = threadIdx.x;
+  const int bucket = part_of(sh, sh.before, sh.places, kBuckets, by_count, at);
+  const uint64_t before = sh.before[bucket];
+  const uint64_t place = counted ? sh.places[bucket] : 0;
+  if (bucket < listed.lo || bucket > listed.hi) {
+    listed.lo = counted && reach && sh.places[bucket + 1] <= kList ? 0 : bucket;
+    listed.hi = bucket;
+    __syncthreads();
+    if (tid == 0) sh.n_list = 0;
+    __syncthreads();
+    row.each([&](float l, int j) {
+      const int b = sc.bucket(l);
+      if (b >= listed.lo && b <= listed.hi) {
+        const uint32_t i = atomicAdd(&sh.n_list, 1u);
+        if (i < kList) sh.list[i] = entry_of(key_of(l), j);
+      }
+    });
+    __syncthreads();
+    listed.n = sh.n_list;
+    if (listed.n > kList) {
+      listed = {0, -1, 0};
+      return among_many(sh, row, sc, bucket, by_count, at, before, place);
+    }
+  }
+  // the bucket's own among the collected
+  if (tid == 0) sh.n_small = 0;
+  __syncthreads();
+  for (uint32_t i = tid; i < listed.n; i += kThreads) {
+    const uint64_t e = sh.list[i];
+    if (sc.bucket(logit_of(static_cast<uint32_t>(e >> 32))) == bucket) {
+      const uint32_t k = atomicAdd(&sh.n_small, 1u);
+      if (k < kSmall) sh.small[k] = e;
+    }
+  }
+  __syncthreads();
+  if (sh.n_small > kSmall) {
+    __syncthreads();
+    listed = {0, -1, 0};
+    return among_many(sh, row, sc, bucket, by_count, at, before, place);
+  }
+  return among_small(sh, sc, by_count, at, before, place);
+}
+
+template <class Row>
+__device__ void sample_row(const SampleArgs& a, Shared& sh, int64_t r) {
+  const int tid = threadIdx.x;
+  const Row row(a.L + r * a.ldl, static_cast<int>(a.vocab));
+  // the first of the largest logits
+  uint64_t best = 0;
+  {
+    uint32_t top = 0, index = 0;
+    row.each([&](float l, int j) {
+      const uint32_t k = key_of(l);
+      if (k > top) {
+        top = k;
+        index = static_cast<uint32_t>(j);
+      }
+    });
+    best = static_cast<uint64_t>(top) << 32 | (0xffffffffu - index);
+    best = block_reduce(best, sh.wave_w, [](uint64_t x, uint64_t y) { return x > y ? x : y; });
+  }
+  const uint32_t top = static_cast<uint32_t>(best >> 32);
+  const float m = logit_of(top);
+  const float T = a.temperature ? a.temperature[r] : 1.0f;
+  int32_t token = -1;
+  float prob = 0.0f;
+  if (top == kNanKey) {
+    prob = __uint_as_float(0x7fc00000u);
+  } else if (a.vocab == 0 || m == -__builtin_inff()) {
+    // nothing to draw
+  } else if (!(T > 0.0f)) {
+    token = static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(best));
+    prob = 1.0f;
+  } else {
+    const Scale sc = {m, 1.0 / static_cast<double>(T)};
+    const float mp = a.min_p ? a.min_p[r] : 0.0f, P = a.top_p ? a.top_p[r] : 1.0f;
+    const int64_t K = a.top_k ? a.top_k[r] : 0;
+    const bool use_k = K > 0 && K < a.vocab, use_p = P < 1.0f, use_m = mp > 0.0f;
+    const double cut = use_m ? (mp >= 1.0f ? 0.0 : log_of(mp)) : 0.0;
+    const bool counted = use_k || use_p;
+    for (int b = tid; b < kBuckets; b += kThreads) {
+      sh.before[b] = 0;
+      sh.places[b] = 0;
+    }
+    for (int b = tid; b < kWeighted; b += kThreads)
+      sh.table[b] = exp43(static_cast<double>(b) * (-1.0 / kPerUnit));
+    __syncthreads();
+    uint64_t near = 0;  // the weight that min_p leaves
+    row.each([&](float l, int) {
+      const double d = sc.d(l);
+      int b = kBuckets - 1;
+      if (Scale::weighs(d)) {
+        const uint64_t w = Scale::weight(sh.table, d, &b);
+        add_u64(&sh.before[b], w);
+        if (use_m && d >= cut) near += w;
+      }
+      if (counted) atomicAdd(&sh.places[b], 1u);
+    });
+    __syncthreads();
+    running(sh, sh.before, sh.places, kBuckets);
+    uint64_t kept = sh.before[kBuckets];
+    if (use_m) near = block_reduce(near, sh.wave_w, [](uint64_t x, uint64_t y) { return x + y; });
+    Listed listed = {0, -1, 0};
+    if (use_k) {
+      const Found f = locate(sh, row, sc, true, static_cast<uint64_t>(K - 1), counted, true, listed);
+      kept = f.before + f.w;
+    }
+    if (use_p) {
+      uint64_t limit = 1;
+      if (P > 0.0f) {
+        const double x = __builtin_ceil(static_cast<double>(P) * static_cast<double>(kept));
+        limit = x < 1.0 ? 1 : static_cast<uint64_t>(x);
+        limit = limit < kept ? limit : kept;
+      }
+      const Found f = locate(sh, row, sc, false, limit - 1, counted, true, listed);
+      kept = f.before + f.w;
+    }
+    if (use_m) kept = near < kept ? near : kept;
+    const float u = a.u[r];
+    uint64_t at = 0;
+    if (u > 0.0f) {
+      if (u >= 1.0f) at = kept - 1;
+      else at = static_cast<uint64_t>(static_cast<double>(u) * static_cast<double>(kept));
+      at = at < kept - 1 ? at : kept - 1;
+    }
+    const Found f = locate(sh, row, sc, false, at, counted, false, listed);
+    token = static_cast<int32_t>(f.index);
+    prob = static_cast<float>(static_cast<double>(f.w) / static_cast<double>(kept));
+  }
+  if (tid == 0) {
+    a.token[r] = token;
+    if (a.prob) a.prob[r] = prob;
+  }
+  __syncthreads();
+}
+
+template <class Row>
+__global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
+  __shared__ Shared sh;
+  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) sample_row<Row>(a, sh, r);
 }
 
 }  // namespace
@@ -382,8 +599,11 @@ uint64_t sample_workspace_bytes(int64_t, int64_t) { return 0; }
 
 hipError_t launch_sample(const SampleArgs& a, void*, hipStream_t s) {
   const int64_t cap = int64_t(1) << 20;
-  hipLaunchKernelGGL(sample_kernel, dim3(static_cast<unsigned>(a.rows < cap ? a.rows : cap)),
-                     dim3(kThreads), 0, s, a);
+  void (*k)(SampleArgs) = sample_kernel<Streamed>;
+  if (a.vocab <= 8 * kThreads) k = sample_kernel<Held<8>>;
+  else if (a.vocab <= 32 * kThreads) k = sample_kernel<Held<32>>;
+  hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(a.rows < cap ? a.rows : cap)), dim3(kThreads), 0,
+                     s, a);
   return hipGetLastError();
 }
 
