@@ -12,11 +12,14 @@
 // The bucket also carries the exponential: with b = rint(-64 d) and r = d + b/64,
 // exp(d) = exp(-b/64) exp(r), |r| <= 1/128, so a table of the first factor (built
 // with the full polynomial) leaves five fused steps per token.  A row is read for
-// its maximum, for the buckets' weights, and for the tokens of the buckets wanted;
-// up to 32768 tokens stay in registers between.
+// its maximum, for the buckets' weights, and for the tokens of the buckets wanted
+// (a float comparison rejects the others); the later reads find it in the caches.
+// (Rows held in registers between the passes measured slower: 1 x 32000 46 us
+// against 28, each token's bounds check standing between the loads.)
 #include <hip/hip_runtime.h>
 
 #include "generation_internal.h"
+#include "row_reduce.h"
 
 #pragma clang fp contract(off)
 
@@ -80,13 +83,11 @@ __device__ double log_of(float m) {
   return __builtin_fma(static_cast<double>(e), 0x1.62e42fefa39efp-1, two_s * p);
 }
 
-// Larger logits have larger keys; -0 and +0 share one.  A NaN's is the largest.
-constexpr uint32_t kNanKey = 0xffffffffu;
+// Larger logits have larger keys; -0 and +0 share one.
 __device__ __forceinline__ uint32_t key_of(float l) {
   uint32_t b = __float_as_uint(l);
   if (b == 0x80000000u) b = 0;
-  b = (b & 0x80000000u) ? ~b : b | 0x80000000u;
-  return l != l ? kNanKey : b;
+  return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float logit_of(uint32_t key) {
   return __uint_as_float((key & 0x80000000u) ? key & 0x7fffffffu : ~key);
@@ -99,8 +100,7 @@ struct Shared {
   union {
     struct {
       uint64_t list[kList];       // (key, ~index): larger comes first in the order
-      uint64_t small[kSmall];
-      uint64_t small_w[kSmall];
+      ulonglong2 small[kSmall];     // the same with their weights
     };
     struct {
       uint64_t sub_w[kSub];
@@ -109,6 +109,7 @@ struct Shared {
   };
   uint64_t wave_w[kWaves];
   uint32_t wave_c[kWaves];
+  float wave_m[kWaves];
   uint64_t found_before, found_w;
   uint32_t found_index, n_list, n_small, lo, hi;
   int found_bucket;
@@ -130,6 +131,18 @@ struct Scale {
   __device__ __forceinline__ int bucket(float l) const {
     const double v = d(l);
     return weighs(v) ? __double2loint(shifted(v)) : kBuckets - 1;
+  }
+  // No logit of buckets 0 .. b is below this: half a bucket beyond the last one's
+  // end, rounded down.
+  __device__ __forceinline__ float least(int b) const {
+    if (b >= kBuckets - 1) return -__builtin_inff();
+    const double v = static_cast<double>(top) - (b + 1.0) / kPerUnit / inverse;
+    float f = static_cast<float>(v);
+    if (static_cast<double>(f) > v) {  // one step down
+      const int32_t i = __float_as_int(f);
+      f = __int_as_float(f > 0.0f ? i - 1 : f < 0.0f ? i + 1 : static_cast<int32_t>(0x80000001u));
+    }
+    return f == f ? f : -__builtin_inff();  // an infinite top or temperature: no bound
   }
   // for d that weighs
   static __device__ __forceinline__ uint64_t weight(const double* table, double d, int* bucket) {
@@ -153,56 +166,36 @@ struct Scale {
   }
 };
 
-// ---------------------------------------------------------------------------
-// A workgroup's view of a row: f(logit, index) for every token, in registers or
-// read again each time.
-// ---------------------------------------------------------------------------
-
-template <int PER>
-struct Held {
-  float v[PER];
-  int n;
-  __device__ __forceinline__ Held(const float* l, int n_) : n(n_) {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int j = static_cast<int>(threadIdx.x) + i * kThreads;
-      v[i] = 0.0f;
-      if (j < n) v[i] = l[j];
-    }
-  }
-  template <class F>
-  __device__ __forceinline__ void each(F f) const {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int j = static_cast<int>(threadIdx.x) + i * kThreads;
-      if (j < n) f(v[i], j);
-    }
-  }
-};
-
-struct Streamed {
+// A workgroup's walk over a row: f(logits, index of the first, how many), four
+// neighbouring tokens at a time (fewer at the end), loads ahead of their use.
+struct Row {
   const float* l;
   int n;
-  __device__ __forceinline__ Streamed(const float* l_, int n_) : l(l_), n(n_) {}
   template <class F>
-  __device__ __forceinline__ void each(F f) const {
-    constexpr int U = 4;  // 16-byte loads in flight (any 4-byte alignment)
+  __device__ __forceinline__ void each4(F f) const {
+    constexpr int U = 4, kStep = kThreads * 4;
     int j = static_cast<int>(threadIdx.x) * 4;
-    for (; j + (U - 1) * kThreads * 4 + 4 <= n; j += U * kThreads * 4) {
-      float4 x[U];
+    for (; j + (U - 1) * kStep + 4 <= n; j += U * kStep) {
+      float x[U][4];
 #pragma unroll
-      for (int u = 0; u < U; ++u) __builtin_memcpy(&x[u], l + j + u * kThreads * 4, 16);
+      for (int u = 0; u < U; ++u) __builtin_memcpy(x[u], l + j + u * kStep, 16);  // any alignment
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int k = j + u * kThreads * 4;
-        f(x[u].x, k);
-        f(x[u].y, k + 1);
-        f(x[u].z, k + 2);
-        f(x[u].w, k + 3);
-      }
+      for (int u = 0; u < U; ++u) f(x[u], j + u * kStep, 4);
     }
-    for (; j < n; j += kThreads * 4)
-      for (int k = j; k < j + 4 && k < n; ++k) f(l[k], k);
+    for (; j < n; j += kStep) {
+      float x[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] = l[j + k < n ? j + k : n - 1];
+      f(x, j, n - j < 4 ? n - j : 4);
+    }
+  }
+  template <class F>
+  __device__ __forceinline__ void each(F f) const {  // f(logit, index)
+    each4([&](const float (&x)[4], int j, int count) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k < count) f(x[k], j + k);
+    });
   }
 };
 
@@ -212,9 +205,20 @@ __device__ T block_reduce(T v, T* per_wave, Op op) {
   if ((threadIdx.x & 63) == 0) per_wave[threadIdx.x >> 6] = v;
   __syncthreads();
   T r = per_wave[0];
+#pragma unroll
   for (int k = 1; k < kWaves; ++k) r = op(r, per_wave[k]);
   __syncthreads();
   return r;
+}
+
+// What stands in the waves before this one.
+template <class T>
+__device__ __forceinline__ T waves_before(const T* per_wave) {
+  const int wave = threadIdx.x >> 6;
+  T sum = 0;
+#pragma unroll
+  for (int k = 0; k < kWaves - 1; ++k) sum += k < wave ? per_wave[k] : T(0);
+  return sum;
 }
 
 __device__ __forceinline__ void add_u64(uint64_t* p, uint64_t v) {
@@ -242,10 +246,8 @@ __device__ void running(Shared& sh, uint64_t* w, uint32_t* c, int buckets) {
     sh.wave_c[wave] = sc;
   }
   __syncthreads();
-  for (int k = 0; k < wave; ++k) {
-    sw += sh.wave_w[k];
-    sc += sh.wave_c[k];
-  }
+  sw += waves_before(sh.wave_w);
+  sc += waves_before(sh.wave_c);
   if (b <= buckets) {
     w[b] = sw - w0 - w1;
     c[b] = sc - c0 - c1;
@@ -288,18 +290,19 @@ __device__ Found among_small(Shared& sh, const Scale& sc, bool by_count, uint64_
   const uint32_t n = sh.n_small, i = threadIdx.x;
   uint64_t mine = 0, w = 0;
   if (i < n) {
-    mine = sh.small[i];
+    mine = sh.small[i].x;
     w = sc.weight(sh.table, logit_of(static_cast<uint32_t>(mine >> 32)));
-    sh.small_w[i] = w;
+    sh.small[i].y = w;
   }
   __syncthreads();
   if (i < n) {
     uint64_t bw = before, bc = place;
-    for (uint32_t o = 0; o < n; ++o)
-      if (sh.small[o] > mine) {
-        bw += sh.small_w[o];
-        ++bc;
-      }
+#pragma unroll 4
+    for (uint32_t o = 0; o < n; ++o) {
+      const ulonglong2 e = sh.small[o];
+      bw += e.x > mine ? e.y : 0;
+      bc += e.x > mine ? 1 : 0;
+    }
     if (by_count ? bc == at : at >= bw && at < bw + w) {
       sh.found_before = bw;
       sh.found_w = w;
@@ -318,7 +321,6 @@ __device__ __forceinline__ uint64_t entry_of(uint32_t key, int j) {
 
 // A bucket with more tokens than kSmall: its keys' interval is cut into kSub parts
 // again and again, until the part that holds `at` is small or a single key.
-template <class Row>
 __device__ Found among_many(Shared& sh, const Row& row, const Scale& sc, int bucket, bool by_count,
                             uint64_t at, uint64_t before, uint64_t place) {
   const int tid = threadIdx.x;
@@ -375,10 +377,8 @@ __device__ Found among_many(Shared& sh, const Row& row, const Scale& sc, int buc
       sh.wave_c[tid >> 6] = bc;
     }
     __syncthreads();
-    for (int k = 0; k < tid >> 6; ++k) {
-      bw += sh.wave_w[k];
-      bc += sh.wave_c[k];
-    }
+    bw += waves_before(sh.wave_w);
+    bc += waves_before(sh.wave_c);
     bw = bw - w + before;
     const uint64_t bp = bc - c + place;
     if (by_count ? at >= bp && at < bp + c : at >= bw && at < bw + w) {
@@ -402,7 +402,7 @@ __device__ Found among_many(Shared& sh, const Row& row, const Scale& sc, int buc
     __syncthreads();
     row.each([&](float l, int j) {
       const uint32_t k = key_of(l);
-      if (k >= lo && k <= hi) sh.small[atomicAdd(&sh.n_small, 1u)] = entry_of(k, j);
+      if (k >= lo && k <= hi) sh.small[atomicAdd(&sh.n_small, 1u)].x = entry_of(k, j);
     });
     __syncthreads();
     return among_small(sh, sc, by_count, at, before, place);
@@ -430,7 +430,7 @@ __device__ Found among_many(Shared& sh, const Row& row, const Scale& sc, int buc
     }
     if ((tid & 63) == 63) sh.wave_c[tid >> 6] = upto;
     __syncthreads();
-    for (int k = 0; k < tid >> 6; ++k) upto += sh.wave_c[k];
+    upto += waves_before(sh.wave_c);
     const uint64_t b = skipped + upto - c;
     if (want >= b && want < b + c) {
       sh.found_bucket = tid;
@@ -448,7 +448,6 @@ __device__ Found among_many(Shared& sh, const Row& row, const Scale& sc, int buc
 // The token at `at` of the order: the first at which the running weight exceeds
 // `at`, or (by_count) the one in that place.  `reach`: also collect the buckets
 // before it, if they fit, for the searches that follow.
-template <class Row>
 __device__ Found locate(Shared& sh, const Row& row, const Scale& sc, bool by_count, uint64_t at,
                         bool counted, bool reach, Listed& listed) {
   const int tid = threadIdx.x;
@@ -461,11 +460,14 @@ __device__ Found locate(Shared& sh, const Row& row, const Scale& sc, bool by_cou
     __syncthreads();
     if (tid == 0) sh.n_list = 0;
     __syncthreads();
+    const float least = sc.least(listed.hi);
     row.each([&](float l, int j) {
-      const int b = sc.bucket(l);
-      if (b >= listed.lo && b <= listed.hi) {
-        const uint32_t i = atomicAdd(&sh.n_list, 1u);
-        if (i < kList) sh.list[i] = entry_of(key_of(l), j);
+      if (l >= least) {
+        const int b = sc.bucket(l);
+        if (b >= listed.lo && b <= listed.hi) {
+          const uint32_t i = atomicAdd(&sh.n_list, 1u);
+          if (i < kList) sh.list[i] = entry_of(key_of(l), j);
+        }
       }
     });
     __syncthreads();
@@ -482,7 +484,7 @@ __device__ Found locate(Shared& sh, const Row& row, const Scale& sc, bool by_cou
     const uint64_t e = sh.list[i];
     if (sc.bucket(logit_of(static_cast<uint32_t>(e >> 32))) == bucket) {
       const uint32_t k = atomicAdd(&sh.n_small, 1u);
-      if (k < kSmall) sh.small[k] = e;
+      if (k < kSmall) sh.small[k].x = e;
     }
   }
   __syncthreads();
@@ -494,40 +496,44 @@ __device__ Found locate(Shared& sh, const Row& row, const Scale& sc, bool by_cou
   return among_small(sh, sc, by_count, at, before, place);
 }
 
-template <class Row>
 __device__ void sample_row(const SampleArgs& a, Shared& sh, int64_t r) {
   const int tid = threadIdx.x;
-  const Row row(a.L + r * a.ldl, static_cast<int>(a.vocab));
-  // the first of the largest logits
-  uint64_t best = 0;
-  {
-    uint32_t top = 0, index = 0;
-    row.each([&](float l, int j) {
-      const uint32_t k = key_of(l);
-      if (k > top) {
-        top = k;
-        index = static_cast<uint32_t>(j);
-      }
-    });
-    best = static_cast<uint64_t>(top) << 32 | (0xffffffffu - index);
-    best = block_reduce(best, sh.wave_w, [](uint64_t x, uint64_t y) { return x > y ? x : y; });
-  }
-  const uint32_t top = static_cast<uint32_t>(best >> 32);
-  const float m = logit_of(top);
+  const Row row = {a.L + r * a.ldl, static_cast<int>(a.vocab)};
   const float T = a.temperature ? a.temperature[r] : 1.0f;
+  const float mp = a.min_p ? a.min_p[r] : 0.0f, P = a.top_p ? a.top_p[r] : 1.0f;
+  const int64_t K = a.top_k ? a.top_k[r] : 0;
+  const float u = a.u[r];
+  // the largest logit
+  float m = -__builtin_inff();
+  bool nan = false;
+  row.each4([&](const float (&x)[4], int, int) {  // (the last one again where fewer are left)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      nan |= x[k] != x[k];
+      m = x[k] > m ? x[k] : m;
+    }
+  });
+  m = wave_max(m);
+  if ((tid & 63) == 0) sh.wave_m[tid >> 6] = m;
+  nan = __syncthreads_or(nan);
+#pragma unroll
+  for (int k = 0; k < kWaves; ++k) m = sh.wave_m[k] > m ? sh.wave_m[k] : m;
   int32_t token = -1;
   float prob = 0.0f;
-  if (top == kNanKey) {
+  if (nan) {
     prob = __uint_as_float(0x7fc00000u);
-  } else if (a.vocab == 0 || m == -__builtin_inff()) {
+  } else if (m == -__builtin_inff()) {
     // nothing to draw
   } else if (!(T > 0.0f)) {
-    token = static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(best));
+    uint32_t first = 0xffffffffu;
+    row.each([&](float l, int j) {
+      if (l == m) first = static_cast<uint32_t>(j) < first ? static_cast<uint32_t>(j) : first;
+    });
+    token = static_cast<int32_t>(block_reduce(
+        first, sh.wave_c, [](uint32_t x, uint32_t y) { return x < y ? x : y; }));
     prob = 1.0f;
   } else {
     const Scale sc = {m, 1.0 / static_cast<double>(T)};
-    const float mp = a.min_p ? a.min_p[r] : 0.0f, P = a.top_p ? a.top_p[r] : 1.0f;
-    const int64_t K = a.top_k ? a.top_k[r] : 0;
     const bool use_k = K > 0 && K < a.vocab, use_p = P < 1.0f, use_m = mp > 0.0f;
     const double cut = use_m ? (mp >= 1.0f ? 0.0 : log_of(mp)) : 0.0;
     const bool counted = use_k || use_p;
@@ -539,20 +545,32 @@ __device__ void sample_row(const SampleArgs& a, Shared& sh, int64_t r) {
       sh.table[b] = exp43(static_cast<double>(b) * (-1.0 / kPerUnit));
     __syncthreads();
     uint64_t near = 0;  // the weight that min_p leaves
-    row.each([&](float l, int) {
-      const double d = sc.d(l);
-      int b = kBuckets - 1;
-      if (Scale::weighs(d)) {
-        const uint64_t w = Scale::weight(sh.table, d, &b);
-        add_u64(&sh.before[b], w);
-        if (use_m && d >= cut) near += w;
+    row.each4([&](const float (&x)[4], int, int count) {
+      uint64_t w[4];
+      int b[4];
+      bool in[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const double d = sc.d(x[k]);
+        in[k] = Scale::weighs(d) && k < count;
+        w[k] = Scale::weight(sh.table, in[k] ? d : 0.0, &b[k]);
+        if (use_m) near += in[k] && d >= cut ? w[k] : 0;
       }
-      if (counted) atomicAdd(&sh.places[b], 1u);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (in[k]) add_u64(&sh.before[b[k]], w[k]);
+      if (counted) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (in[k]) atomicAdd(&sh.places[b[k]], 1u);
+      }
     });
     __syncthreads();
     running(sh, sh.before, sh.places, kBuckets);
+    if (tid == 0) sh.places[kBuckets] = static_cast<uint32_t>(a.vocab);  // with those of no weight
     uint64_t kept = sh.before[kBuckets];
     if (use_m) near = block_reduce(near, sh.wave_w, [](uint64_t x, uint64_t y) { return x + y; });
+    __syncthreads();
     Listed listed = {0, -1, 0};
     if (use_k) {
       const Found f = locate(sh, row, sc, true, static_cast<uint64_t>(K - 1), counted, true, listed);
@@ -569,7 +587,6 @@ __device__ void sample_row(const SampleArgs& a, Shared& sh, int64_t r) {
       kept = f.before + f.w;
     }
     if (use_m) kept = near < kept ? near : kept;
-    const float u = a.u[r];
     uint64_t at = 0;
     if (u > 0.0f) {
       if (u >= 1.0f) at = kept - 1;
@@ -587,10 +604,9 @@ __device__ void sample_row(const SampleArgs& a, Shared& sh, int64_t r) {
   __syncthreads();
 }
 
-template <class Row>
 __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
   __shared__ Shared sh;
-  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) sample_row<Row>(a, sh, r);
+  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) sample_row(a, sh, r);
 }
 
 }  // namespace
@@ -599,10 +615,7 @@ uint64_t sample_workspace_bytes(int64_t, int64_t) { return 0; }
 
 hipError_t launch_sample(const SampleArgs& a, void*, hipStream_t s) {
   const int64_t cap = int64_t(1) << 20;
-  void (*k)(SampleArgs) = sample_kernel<Streamed>;
-  if (a.vocab <= 8 * kThreads) k = sample_kernel<Held<8>>;
-  else if (a.vocab <= 32 * kThreads) k = sample_kernel<Held<32>>;
-  hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(a.rows < cap ? a.rows : cap)), dim3(kThreads), 0,
+  hipLaunchKernelGGL(sample_kernel, dim3(static_cast<unsigned>(a.rows < cap ? a.rows : cap)), dim3(kThreads), 0,
                      s, a);
   return hipGetLastError();
 }
