@@ -11,11 +11,14 @@
 //
 // The bucket also carries the exponential: with b = rint(-64 d) and r = d + b/64,
 // exp(d) = exp(-b/64) exp(r), |r| <= 1/128, so a table of the first factor (built
-// with the full polynomial) leaves five fused steps per token.  A row is read for
-// its maximum, for the buckets' weights, and for the tokens of the buckets wanted
-// (a float comparison rejects the others); the later reads find it in the caches.
-// (Rows held in registers between the passes measured slower: 1 x 32000 46 us
-// against 28, each token's bounds check standing between the loads.)
+// with the full polynomial) leaves five fused steps per token.
+//
+// A row is walked for its maximum, for the buckets' weights and for the tokens of the
+// buckets wanted (a float comparison rejects most others).  The second walk is bound by
+// instruction issue (about 35 a token), the others by memory.  Rows of up to 16384
+// tokens take one workgroup and one launch; longer ones a launch for each walk, the
+// first two with several workgroups a row where rows are few, in groups of rows whose
+// logits stay in the 256 MB cache from one walk to the next.
 #include <hip/hip_runtime.h>
 
 #include "generation_internal.h"
@@ -26,13 +29,13 @@
 namespace repops {
 namespace {
 
-constexpr int kThreads = 1024;
-constexpr int kWaves = kThreads / 64;
+constexpr int kThreads = 1024;       // of the workgroup that picks a row's token
+constexpr int kWeighThreads = 512;   // of those that share a long row's first walks
 constexpr double kSpan = 31.0;        // exp(-31) < 2^-44: a weight of 0
 constexpr int kPerUnit = 64;          // buckets per unit of d
 constexpr int kWeighted = 31 * kPerUnit + 1;  // buckets 0 .. 1984: rint(64 * 31)
 constexpr int kBuckets = kWeighted + 1;       // the last one: weight 0
-constexpr int kList = 2048;           // tokens collected at once
+constexpr int kList = 4096;           // tokens collected at once
 constexpr int kSmall = kThreads;      // tokens put in order at once
 constexpr int kSub = 1024;            // parts that a bucket's keys are narrowed by
 
@@ -56,6 +59,11 @@ __device__ __forceinline__ double exp43(double d) {
   p = __builtin_fma(p, r, 1.0);
   p = __builtin_fma(p, r, 1.0);
   return p * __hiloint2double((1023 + 43 + static_cast<int>(n)) << 20, 0);  // exact
+}
+
+// exp(-b / 64) 2^43
+__device__ __forceinline__ double table_entry(int b) {
+  return exp43(static_cast<double>(b) * (-1.0 / kPerUnit));
 }
 
 // Natural logarithm of m in (0, 1).
@@ -93,31 +101,36 @@ __device__ __forceinline__ float logit_of(uint32_t key) {
   return __uint_as_float((key & 0x80000000u) ? key & 0x7fffffffu : ~key);
 }
 
-struct Shared {
+// What a row's second walk fills.
+struct Weights {
   uint64_t before[kBuckets + 1];  // weights per bucket, then the running weight before each
   uint32_t places[kBuckets + 1];  // counts likewise
-  double table[kWeighted];        // exp(-b / 64) 2^43
+  uint64_t wave_w[16];
+  uint32_t wave_c[16];
+  float wave_m[16];
+};
+
+struct Shared : Weights {
   union {
+    double table[kWeighted];     // second walk: exp(-b / 64) 2^43
     struct {
-      uint64_t list[kList];       // (key, ~index): larger comes first in the order
-      ulonglong2 small[kSmall];     // the same with their weights
+      uint64_t list[kList];      // (key, ~index): larger comes first in the order
+      ulonglong2 small[kSmall];  // the same with their weights
     };
     struct {
       uint64_t sub_w[kSub];
       uint32_t sub_c[kSub];
     };
   };
-  uint64_t wave_w[kWaves];
-  uint32_t wave_c[kWaves];
-  float wave_m[kWaves];
   uint64_t found_before, found_w;
-  uint32_t found_index, n_list, n_small, lo, hi;
+  uint32_t found_index, n_small, n_list, lo, hi;
   int found_bucket;
 };
 
 // Where a logit stands: d, its bucket and, asked for, its weight.
 struct Scale {
   float top;       // the row's largest logit
+  float temperature;
   double inverse;  // 1 / temperature
   __device__ __forceinline__ double d(float l) const {
     const double v = (static_cast<double>(l) - static_cast<double>(top)) * inverse;
@@ -132,22 +145,12 @@ struct Scale {
     const double v = d(l);
     return weighs(v) ? __double2loint(shifted(v)) : kBuckets - 1;
   }
-  // No logit of buckets 0 .. b is below this: half a bucket beyond the last one's
-  // end, rounded down.
-  __device__ __forceinline__ float least(int b) const {
-    if (b >= kBuckets - 1) return -__builtin_inff();
-    const double v = static_cast<double>(top) - (b + 1.0) / kPerUnit / inverse;
-    float f = static_cast<float>(v);
-    if (static_cast<double>(f) > v) {  // one step down
-      const int32_t i = __float_as_int(f);
-      f = __int_as_float(f > 0.0f ? i - 1 : f < 0.0f ? i + 1 : static_cast<int32_t>(0x80000001u));
-    }
-    return f == f ? f : -__builtin_inff();  // an infinite top or temperature: no bound
-  }
-  // for d that weighs
-  static __device__ __forceinline__ uint64_t weight(const double* table, double d, int* bucket) {
+  // For d that weighs; entry(b): exp(-b / 64) 2^43, from the table or computed.
+  template <class Entry>
+  static __device__ __forceinline__ uint64_t weight(Entry entry, double d, int* bucket) {
     const double t = shifted(d);
     *bucket = __double2loint(t);
+    const double e = entry(*bucket);
     const double r = __builtin_fma(t - 0x1p52, 1.0 / kPerUnit, d);
     double p = 0x1.1111111111111p-7;  // 1/5!
     p = __builtin_fma(p, r, 0x1.5555555555555p-5);
@@ -156,32 +159,39 @@ struct Scale {
     p = __builtin_fma(p, r, 1.0);
     p = __builtin_fma(p, r, 1.0);
     // adding 2^52 rounds to an integer (ties to even)
-    const double w = __builtin_fma(table[*bucket], p, 0x1p52);
+    const double w = __builtin_fma(e, p, 0x1p52);
     return static_cast<uint64_t>(__double_as_longlong(w)) & 0xfffffffffffffull;
   }
-  __device__ __forceinline__ uint64_t weight(const double* table, float l) const {
+  __device__ __forceinline__ uint64_t weight(float l) const {
     const double v = d(l);
     int b;
-    return weighs(v) ? weight(table, v, &b) : 0;
+    return weighs(v) ? weight(table_entry, v, &b) : 0;
   }
 };
 
-// A workgroup's walk over a row: f(logits, index of the first, how many), four
-// neighbouring tokens at a time (fewer at the end), loads ahead of their use.
+// The walk of a workgroup of NT threads over a row, or over a stretch of one.
+template <int NT>
 struct Row {
   const float* l;
   int n;
-  template <class F>
+  // f(logits, index of the first, how many) for four neighbouring tokens at a time
+  // (fewer at the end), loads ahead of their use.
+  template <int U, class F>
   __device__ __forceinline__ void each4(F f) const {
-    constexpr int U = 4, kStep = kThreads * 4;
+    constexpr int kStep = NT * 4;
     int j = static_cast<int>(threadIdx.x) * 4;
+#pragma nounroll
     for (; j + (U - 1) * kStep + 4 <= n; j += U * kStep) {
       float x[U][4];
+      // (32-bit offsets from the row's uniform address; any alignment)
+      const char* at = reinterpret_cast<const char*>(l);
+      const uint32_t off = static_cast<uint32_t>(j) * 4u;
 #pragma unroll
-      for (int u = 0; u < U; ++u) __builtin_memcpy(x[u], l + j + u * kStep, 16);  // any alignment
+      for (int u = 0; u < U; ++u) __builtin_memcpy(x[u], at + (off + u * (kStep * 4u)), 16);
 #pragma unroll
       for (int u = 0; u < U; ++u) f(x[u], j + u * kStep, 4);
     }
+#pragma nounroll
     for (; j < n; j += kStep) {
       float x[4];
 #pragma unroll
@@ -189,24 +199,22 @@ struct Row {
       f(x, j, n - j < 4 ? n - j : 4);
     }
   }
+  // f(logit, index) for every token, one at a time.
   template <class F>
-  __device__ __forceinline__ void each(F f) const {  // f(logit, index)
-    each4([&](const float (&x)[4], int j, int count) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (k < count) f(x[k], j + k);
-    });
+  __device__ __forceinline__ void each(F f) const {
+#pragma nounroll
+    for (int j = static_cast<int>(threadIdx.x); j < n; j += NT) f(l[j], j);
   }
 };
 
-template <class T, class Op>
+template <int NT, class T, class Op>
 __device__ T block_reduce(T v, T* per_wave, Op op) {
   for (int s = 32; s >= 1; s >>= 1) v = op(v, __shfl_xor(v, s));
   if ((threadIdx.x & 63) == 0) per_wave[threadIdx.x >> 6] = v;
   __syncthreads();
   T r = per_wave[0];
 #pragma unroll
-  for (int k = 1; k < kWaves; ++k) r = op(r, per_wave[k]);
+  for (int k = 1; k < NT / 64; ++k) r = op(r, per_wave[k]);
   __syncthreads();
   return r;
 }
@@ -217,7 +225,7 @@ __device__ __forceinline__ T waves_before(const T* per_wave) {
   const int wave = threadIdx.x >> 6;
   T sum = 0;
 #pragma unroll
-  for (int k = 0; k < kWaves - 1; ++k) sum += k < wave ? per_wave[k] : T(0);
+  for (int k = 0; k < kThreads / 64 - 1; ++k) sum += k < wave ? per_wave[k] : T(0);
   return sum;
 }
 
@@ -276,10 +284,36 @@ struct Found {
   uint32_t index;
 };
 
-// Collected tokens: those of the buckets lo .. hi.
+// Holds for every logit of buckets lo .. hi, and for few others: |l - middle| within
+// the buckets' half width, with half a bucket and the rounding to spare.
+struct Interval {
+  float middle, half;
+  __device__ __forceinline__ Interval(const Scale& sc, int lo, int hi) {
+    const double step = static_cast<double>(sc.temperature) / kPerUnit;
+    const double mid = static_cast<double>(sc.top) - 0.5 * (lo + hi) * step;
+    const double wide = (0.5 * (hi - lo) + 1.0) * step;
+    middle = static_cast<float>(mid);
+    // 2^-20 of the larger operand covers the rounding of both and of l - middle
+    half = static_cast<float>((wide + __builtin_fabs(mid)) * 0x1p-20 + wide);
+    // no bound where the weightless bucket is wanted or anything overflows
+    if (hi >= kBuckets - 1 || !(half < __builtin_inff()) || !(__builtin_fabs(mid) < 0x1p127)) {
+      middle = 0.0f;
+      half = __builtin_inff();
+    }
+  }
+  __device__ __forceinline__ bool operator()(float l) const {
+    return !(__builtin_fabsf(l - middle) > half);
+  }
+};
+
+// Collected tokens: those of the buckets lo .. hi and, with the same walk, of
+// lo2 .. hi2 before them (and some of their neighbours').
 struct Listed {
-  int lo, hi;
+  int lo, hi, lo2, hi2;
   uint32_t n;
+  __device__ __forceinline__ bool holds(int b) const {
+    return (b >= lo && b <= hi) || (b >= lo2 && b <= hi2);
+  }
 };
 
 // The token at `at` (weight or place before it) among the sh.n_small tokens of
@@ -291,7 +325,7 @@ __device__ Found among_small(Shared& sh, const Scale& sc, bool by_count, uint64_
   uint64_t mine = 0, w = 0;
   if (i < n) {
     mine = sh.small[i].x;
-    w = sc.weight(sh.table, logit_of(static_cast<uint32_t>(mine >> 32)));
+    w = sc.weight(logit_of(static_cast<uint32_t>(mine >> 32)));
     sh.small[i].y = w;
   }
   __syncthreads();
@@ -321,7 +355,7 @@ __device__ __forceinline__ uint64_t entry_of(uint32_t key, int j) {
 
 // A bucket with more tokens than kSmall: its keys' interval is cut into kSub parts
 // again and again, until the part that holds `at` is small or a single key.
-__device__ Found among_many(Shared& sh, const Row& row, const Scale& sc, int bucket, bool by_count,
+__device__ __noinline__ Found among_many(Shared& sh, const Row<kThreads>& row, const Scale& sc, int bucket, bool by_count,
                             uint64_t at, uint64_t before, uint64_t place) {
   const int tid = threadIdx.x;
   if (tid == 0) {
@@ -355,7 +389,7 @@ __device__ Found among_many(Shared& sh, const Row& row, const Scale& sc, int buc
       if (k >= lo && k <= hi) {
         const uint32_t b = (hi - k) >> shift;
         atomicAdd(&sh.sub_c[b], 1u);
-        add_u64(&sh.sub_w[b], sc.weight(sh.table, l));
+        add_u64(&sh.sub_w[b], sc.weight(l));
       }
     });
     __syncthreads();
@@ -409,7 +443,7 @@ __device__ Found among_many(Shared& sh, const Row& row, const Scale& sc, int buc
   }
   // Equal logits, as many as there are: the place among them in order of the index.
   // The indices are cut into kSub parts in the same way.
-  const uint64_t w = sc.weight(sh.table, logit_of(lo));
+  const uint64_t w = sc.weight(logit_of(lo));
   const uint64_t want = by_count ? at - place : (at - before) / w;
   uint32_t first = 0, span = static_cast<uint32_t>(row.n);
   uint64_t skipped = 0;
@@ -445,35 +479,69 @@ __device__ Found among_many(Shared& sh, const Row& row, const Scale& sc, int buc
   return {before + want * w, w, first};
 }
 
+// The tokens that `in` takes, at most four a thread at a time, into the list (as far
+// as they fit); sh.n_list counts them.
+template <class In>
+__device__ __forceinline__ void collect(Shared& sh, const Row<kThreads>& row, In in) {
+  row.each4<4>([&](const float (&x)[4], int j, int count) {
+    uint32_t taken = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) taken += k < count && in(x[k]);
+    if (taken) {
+      uint32_t i = atomicAdd(&sh.n_list, taken);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k < count && in(x[k])) {
+          if (i < kList) sh.list[i] = entry_of(key_of(x[k]), j + k);
+          ++i;
+        }
+    }
+  });
+}
+
 // The token at `at` of the order: the first at which the running weight exceeds
-// `at`, or (by_count) the one in that place.  `reach`: also collect the buckets
-// before it, if they fit, for the searches that follow.
-__device__ Found locate(Shared& sh, const Row& row, const Scale& sc, bool by_count, uint64_t at,
-                        bool counted, bool reach, Listed& listed) {
+// `at`, or (by_count) the one in that place.  Its bucket is collected unless it is
+// already, together with what the searches that follow are known to want: with
+// `reach`, all buckets before it, if they fit, else those that hold share * W for the
+// weights W that may yet turn out to be kept (of `bucket` and `near`).
+__device__ Found locate(Shared& sh, const Row<kThreads>& row, const Scale& sc, bool by_count,
+                        uint64_t at, bool counted, bool reach, double share, uint64_t near,
+                        Listed& listed) {
   const int tid = threadIdx.x;
   const int bucket = part_of(sh, sh.before, sh.places, kBuckets, by_count, at);
   const uint64_t before = sh.before[bucket];
   const uint64_t place = counted ? sh.places[bucket] : 0;
-  if (bucket < listed.lo || bucket > listed.hi) {
-    listed.lo = counted && reach && sh.places[bucket + 1] <= kList ? 0 : bucket;
-    listed.hi = bucket;
-    __syncthreads();
+  if (!listed.holds(bucket)) {
+    listed = {bucket, bucket, 0, -1, 0};
+    const int beyond = bucket + 3 < kBuckets ? bucket + 3 : kBuckets;  // past the neighbours'
+    if (reach && sh.places[beyond] <= kList) {
+      listed.lo = 0;
+    } else if (reach && !by_count) {
+      const uint64_t after = sh.before[bucket + 1];
+      const double least = share * static_cast<double>(before < near ? before : near);
+      const double most = share * static_cast<double>(after < near ? after : near);
+      const uint64_t first = static_cast<uint64_t>(least);
+      const int lo2 = part_of(sh, sh.before, sh.places, kBuckets, false,
+                              first < after ? first : after - 1);
+      const uint64_t last = static_cast<uint64_t>(most);
+      const int hi2 = part_of(sh, sh.before, sh.places, kBuckets, false,
+                              last < after ? last : after - 1);
+      listed.lo2 = lo2;
+      listed.hi2 = hi2 < bucket ? hi2 : bucket - 1;
+    }
     if (tid == 0) sh.n_list = 0;
     __syncthreads();
-    const float least = sc.least(listed.hi);
-    row.each([&](float l, int j) {
-      if (l >= least) {
-        const int b = sc.bucket(l);
-        if (b >= listed.lo && b <= listed.hi) {
-          const uint32_t i = atomicAdd(&sh.n_list, 1u);
-          if (i < kList) sh.list[i] = entry_of(key_of(l), j);
-        }
-      }
-    });
+    const Interval one = {sc, listed.lo, listed.hi};
+    if (listed.hi2 < listed.lo2) {
+      collect(sh, row, one);
+    } else {
+      const Interval two = {sc, listed.lo2, listed.hi2};
+      collect(sh, row, [&](float l) { return one(l) || two(l); });
+    }
     __syncthreads();
     listed.n = sh.n_list;
     if (listed.n > kList) {
-      listed = {0, -1, 0};
+      listed = {0, -1, 0, -1, 0};
       return among_many(sh, row, sc, bucket, by_count, at, before, place);
     }
   }
@@ -490,23 +558,37 @@ __device__ Found locate(Shared& sh, const Row& row, const Scale& sc, bool by_cou
   __syncthreads();
   if (sh.n_small > kSmall) {
     __syncthreads();
-    listed = {0, -1, 0};
+    listed = {0, -1, 0, -1, 0};
     return among_many(sh, row, sc, bucket, by_count, at, before, place);
   }
   return among_small(sh, sc, by_count, at, before, place);
 }
 
-__device__ void sample_row(const SampleArgs& a, Shared& sh, int64_t r) {
+// A row's parameters.
+struct Params {
+  float temperature, top_p, min_p, u;
+  int top_k;
+  __device__ __forceinline__ Params(const SampleArgs& a, int64_t r)
+      : temperature(a.temperature ? a.temperature[r] : 1.0f),
+        top_p(a.top_p ? a.top_p[r] : 1.0f),
+        min_p(a.min_p ? a.min_p[r] : 0.0f),
+        u(a.u[r]),
+        top_k(a.top_k ? a.top_k[r] : 0) {}
+  __device__ __forceinline__ double share() const { return u > 0.0f ? u < 1.0f ? u : 1.0 : 0.0; }
+  __device__ __forceinline__ bool greedy() const { return !(temperature > 0.0f); }
+  __device__ __forceinline__ bool use_k(int64_t n) const { return top_k > 0 && top_k < n; }
+  __device__ __forceinline__ bool use_p() const { return top_p < 1.0f; }
+  __device__ __forceinline__ bool use_m() const { return min_p > 0.0f; }
+  __device__ __forceinline__ bool counted(int64_t n) const { return use_k(n) || use_p(); }
+};
+
+// First walk: the largest logit, NaN where one is there, -infinity of none.
+template <int NT>
+__device__ float find_top(const Row<NT>& row, float* wave_m) {
   const int tid = threadIdx.x;
-  const Row row = {a.L + r * a.ldl, static_cast<int>(a.vocab)};
-  const float T = a.temperature ? a.temperature[r] : 1.0f;
-  const float mp = a.min_p ? a.min_p[r] : 0.0f, P = a.top_p ? a.top_p[r] : 1.0f;
-  const int64_t K = a.top_k ? a.top_k[r] : 0;
-  const float u = a.u[r];
-  // the largest logit
   float m = -__builtin_inff();
   bool nan = false;
-  row.each4([&](const float (&x)[4], int, int) {  // (the last one again where fewer are left)
+  row.template each4<4>([&](const float (&x)[4], int, int) {  // (the last again at the end)
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       nan |= x[k] != x[k];
@@ -514,110 +596,286 @@ __device__ void sample_row(const SampleArgs& a, Shared& sh, int64_t r) {
     }
   });
   m = wave_max(m);
-  if ((tid & 63) == 0) sh.wave_m[tid >> 6] = m;
+  if ((tid & 63) == 0) wave_m[tid >> 6] = m;
   nan = __syncthreads_or(nan);
 #pragma unroll
-  for (int k = 0; k < kWaves; ++k) m = sh.wave_m[k] > m ? sh.wave_m[k] : m;
-  int32_t token = -1;
-  float prob = 0.0f;
-  if (nan) {
-    prob = __uint_as_float(0x7fc00000u);
-  } else if (m == -__builtin_inff()) {
-    // nothing to draw
-  } else if (!(T > 0.0f)) {
-    uint32_t first = 0xffffffffu;
-    row.each([&](float l, int j) {
-      if (l == m) first = static_cast<uint32_t>(j) < first ? static_cast<uint32_t>(j) : first;
-    });
-    token = static_cast<int32_t>(block_reduce(
-        first, sh.wave_c, [](uint32_t x, uint32_t y) { return x < y ? x : y; }));
-    prob = 1.0f;
-  } else {
-    const Scale sc = {m, 1.0 / static_cast<double>(T)};
-    const bool use_k = K > 0 && K < a.vocab, use_p = P < 1.0f, use_m = mp > 0.0f;
-    const double cut = use_m ? (mp >= 1.0f ? 0.0 : log_of(mp)) : 0.0;
-    const bool counted = use_k || use_p;
-    for (int b = tid; b < kBuckets; b += kThreads) {
-      sh.before[b] = 0;
-      sh.places[b] = 0;
-    }
-    for (int b = tid; b < kWeighted; b += kThreads)
-      sh.table[b] = exp43(static_cast<double>(b) * (-1.0 / kPerUnit));
-    __syncthreads();
-    uint64_t near = 0;  // the weight that min_p leaves
-    row.each4([&](const float (&x)[4], int, int count) {
-      uint64_t w[4];
-      int b[4];
-      bool in[4];
+  for (int k = 0; k < NT / 64; ++k) m = wave_m[k] > m ? wave_m[k] : m;
+  return nan ? __builtin_nanf("") : m;
+}
+
+// Second walk: the buckets' weights (and counts) into sh, and the weight of the
+// tokens that min_p leaves.
+template <int NT>
+__device__ uint64_t weigh(Weights& sh, double* table, const Row<NT>& row, const Params& p,
+                          const Scale& sc, bool counted) {
+  const int tid = threadIdx.x;
+  const bool use_m = p.use_m();
+  const double cut = use_m ? (p.min_p >= 1.0f ? 0.0 : log_of(p.min_p)) : 0.0;
+#pragma nounroll
+  for (int b = tid; b < kBuckets + 1; b += NT) {
+    sh.before[b] = 0;
+    sh.places[b] = 0;
+  }
+#pragma nounroll
+  for (int b = tid; b < kWeighted; b += NT)
+    table[b] = table_entry(b);
+  __syncthreads();
+  uint64_t near = 0;
+  row.template each4<2>([&](const float (&x)[4], int, int count) {
+    uint64_t w[4];
+    int b[4];
+    bool in[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const double d = sc.d(x[k]);
-        in[k] = Scale::weighs(d) && k < count;
-        w[k] = Scale::weight(sh.table, in[k] ? d : 0.0, &b[k]);
-        if (use_m) near += in[k] && d >= cut ? w[k] : 0;
-      }
+    for (int k = 0; k < 4; ++k) {
+      const double d = sc.d(x[k]);
+      in[k] = Scale::weighs(d) && k < count;
+      w[k] = Scale::weight([&](int e) { return table[e]; }, in[k] ? d : 0.0, &b[k]);
+      if (use_m) near += in[k] && d >= cut ? w[k] : 0;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (in[k]) add_u64(&sh.before[b[k]], w[k]);
+    if (counted) {
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        if (in[k]) add_u64(&sh.before[b[k]], w[k]);
-      if (counted) {
+        if (in[k]) atomicAdd(&sh.places[b[k]], 1u);
+    }
+  });
+  __syncthreads();
+  if (use_m)
+    near = block_reduce<NT>(near, sh.wave_w, [](uint64_t x, uint64_t y) { return x + y; });
+  return near;
+}
+
+// The rest: from a row's weights, the filters' ends and the draw.
+__device__ void pick(const SampleArgs& a, Shared& sh, int64_t r, const Params& p, const Scale& sc,
+                     uint64_t near) {
+  const int tid = threadIdx.x;
+  const Row<kThreads> row = {a.L + r * a.ldl, static_cast<int>(a.vocab)};
+  const bool use_k = p.use_k(a.vocab), use_p = p.use_p(), counted = p.counted(a.vocab);
+  running(sh, sh.before, sh.places, kBuckets);
+  if (tid == 0) sh.places[kBuckets] = static_cast<uint32_t>(a.vocab);  // with those of no weight
+  uint64_t kept = sh.before[kBuckets];
+  __syncthreads();
+  Listed listed = {0, -1, 0, -1, 0};
+  // top_k's end, top_p's end, the draw: one search each
+#pragma nounroll
+  for (int stage = use_k ? 0 : use_p ? 1 : 2; stage < 3; stage += stage == 0 && !use_p ? 2 : 1) {
+    uint64_t at = 0;
+    if (stage == 0) {
+      at = static_cast<uint64_t>(p.top_k - 1);
+    } else if (stage == 1) {
+      if (p.top_p > 0.0f) {
+        const double x = __builtin_ceil(static_cast<double>(p.top_p) * static_cast<double>(kept));
+        at = x < 1.0 ? 0 : static_cast<uint64_t>(x) - 1;
+      }
+    } else {
+      if (p.use_m()) kept = near < kept ? near : kept;
+      at = static_cast<uint64_t>(p.share() * static_cast<double>(kept));
+    }
+    if (stage > 0) at = at < kept - 1 ? at : kept - 1;
+    const Found f = locate(sh, row, sc, stage == 0, at, counted, stage < 2, p.share(),
+                           p.use_m() ? near : ~uint64_t(0), listed);
+    if (stage < 2) {
+      kept = f.before + f.w;
+    } else if (tid == 0) {
+      a.token[r] = static_cast<int32_t>(f.index);
+      if (a.prob)
+        a.prob[r] = static_cast<float>(static_cast<double>(f.w) / static_cast<double>(kept));
+    }
+  }
+}
+
+// A row that needs no weights, given its largest logit: one without a token, one
+// with a NaN, or the first of the largest logits.
+__device__ bool pick_plain(const SampleArgs& a, uint32_t* wave_c, int64_t r, const Params& p,
+                           float m) {
+  int32_t token = -1;
+  float prob = m != m ? m : 0.0f;
+  if (m > -__builtin_inff()) {
+    if (!p.greedy()) return false;
+    const Row<kThreads> row = {a.L + r * a.ldl, static_cast<int>(a.vocab)};
+    uint32_t first = 0xffffffffu;
+    row.each4<4>([&](const float (&x)[4], int j, int count) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (in[k]) atomicAdd(&sh.places[b[k]], 1u);
+      for (int k = 3; k >= 0; --k) {  // (j grows from one call to the next)
+        const uint32_t at = static_cast<uint32_t>(j + k);
+        if (x[k] == m && k < count && at < first) first = at;
       }
     });
-    __syncthreads();
-    running(sh, sh.before, sh.places, kBuckets);
-    if (tid == 0) sh.places[kBuckets] = static_cast<uint32_t>(a.vocab);  // with those of no weight
-    uint64_t kept = sh.before[kBuckets];
-    if (use_m) near = block_reduce(near, sh.wave_w, [](uint64_t x, uint64_t y) { return x + y; });
-    __syncthreads();
-    Listed listed = {0, -1, 0};
-    if (use_k) {
-      const Found f = locate(sh, row, sc, true, static_cast<uint64_t>(K - 1), counted, true, listed);
-      kept = f.before + f.w;
-    }
-    if (use_p) {
-      uint64_t limit = 1;
-      if (P > 0.0f) {
-        const double x = __builtin_ceil(static_cast<double>(P) * static_cast<double>(kept));
-        limit = x < 1.0 ? 1 : static_cast<uint64_t>(x);
-        limit = limit < kept ? limit : kept;
-      }
-      const Found f = locate(sh, row, sc, false, limit - 1, counted, true, listed);
-      kept = f.before + f.w;
-    }
-    if (use_m) kept = near < kept ? near : kept;
-    uint64_t at = 0;
-    if (u > 0.0f) {
-      if (u >= 1.0f) at = kept - 1;
-      else at = static_cast<uint64_t>(static_cast<double>(u) * static_cast<double>(kept));
-      at = at < kept - 1 ? at : kept - 1;
-    }
-    const Found f = locate(sh, row, sc, false, at, counted, false, listed);
-    token = static_cast<int32_t>(f.index);
-    prob = static_cast<float>(static_cast<double>(f.w) / static_cast<double>(kept));
+    token = static_cast<int32_t>(block_reduce<kThreads>(
+        first, wave_c, [](uint32_t x, uint32_t y) { return x < y ? x : y; }));
+    prob = 1.0f;
   }
-  if (tid == 0) {
+  if (threadIdx.x == 0) {
     a.token[r] = token;
     if (a.prob) a.prob[r] = prob;
   }
-  __syncthreads();
+  return true;
 }
 
+__device__ __forceinline__ Scale scale_of(const Params& p, float m) {
+  return {m, p.temperature, 1.0 / static_cast<double>(p.temperature)};
+}
+
+// One workgroup a row.
 __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
   __shared__ Shared sh;
-  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) sample_row(a, sh, r);
+  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+    const Row<kThreads> row = {a.L + r * a.ldl, static_cast<int>(a.vocab)};
+    const Params p(a, r);
+    const float m = find_top(row, sh.wave_m);
+    if (!pick_plain(a, sh.wave_c, r, p, m)) {
+      const Scale sc = scale_of(p, m);
+      const uint64_t near = weigh(sh, sh.table, row, p, sc, p.counted(a.vocab));
+      pick(a, sh, r, p, sc, near);
+    }
+    __syncthreads();  // what the next row overwrites has been read
+  }
 }
+
+// Long rows: a stretch of `stretch` tokens of a row per workgroup in the first two
+// walks, each leaving its part in the workspace.
+struct Part {
+  uint64_t weight[kBuckets];
+  uint64_t near;
+  uint32_t count[kBuckets];
+  float top;
+  uint32_t unused;
+};
+
+__device__ __forceinline__ Row<kWeighThreads> stretch_of(const SampleArgs& a, int64_t r, int g,
+                                                         int stretch) {
+  const int64_t j0 = static_cast<int64_t>(g) * stretch;
+  const int64_t left = a.vocab - j0;
+  return {a.L + r * a.ldl + j0, static_cast<int>(left < stretch ? left : stretch)};
+}
+
+__global__ __launch_bounds__(kWeighThreads) void sample_top_kernel(SampleArgs a, Part* parts,
+                                                                   int G, int stretch) {
+  __shared__ float wave_m[kWeighThreads / 64];
+  const int64_t r = blockIdx.x / G;
+  const float m = find_top(stretch_of(a, r, blockIdx.x % G, stretch), wave_m);
+  if (threadIdx.x == 0) parts[blockIdx.x].top = m;
+}
+
+// The largest of a row's parts' logits (at most 64), NaN where one is there.  Every
+// wave reads them all, a lane each.
+__device__ __forceinline__ float top_of(const Part* parts, int G) {
+  const int lane = threadIdx.x & 63;
+  const float t = lane < G ? parts[lane].top : -__builtin_inff();
+  return __any(t != t) ? __builtin_nanf("") : wave_max(t);
+}
+
+__global__ __launch_bounds__(kWeighThreads) void sample_weigh_kernel(SampleArgs a, Part* parts,
+                                                                     int G, int stretch) {
+  __shared__ Weights sh;
+  __shared__ double table[kWeighted];
+  const int64_t r = blockIdx.x / G;
+  const Params p(a, r);
+  const float m = top_of(parts + r * G, G);
+  if (!(m > -__builtin_inff()) || p.greedy()) return;
+  Part& part = parts[blockIdx.x];
+  const bool counted = p.counted(a.vocab);
+  const uint64_t near =
+      weigh(sh, table, stretch_of(a, r, blockIdx.x % G, stretch), p, scale_of(p, m), counted);
+  for (int b = threadIdx.x; b < kBuckets; b += kWeighThreads) {
+    part.weight[b] = sh.before[b];
+    if (counted) part.count[b] = sh.places[b];
+  }
+  if (threadIdx.x == 0) part.near = near;
+}
+
+__global__ __launch_bounds__(kThreads) void sample_pick_kernel(SampleArgs a, const Part* parts,
+                                                               int G) {
+  __shared__ Shared sh;
+  const int64_t r = blockIdx.x;
+  const Part* part = parts + r * G;
+  const Params p(a, r);
+  const float m = top_of(part, G);
+  if (pick_plain(a, sh.wave_c, r, p, m)) return;
+  const bool counted = p.counted(a.vocab);
+  for (int b = threadIdx.x; b < kBuckets; b += kThreads) {
+    uint64_t w = 0;
+    uint32_t c = 0;
+    if (counted) {
+#pragma unroll 8
+      for (int g = 0; g < G; ++g) c += part[g].count[b];
+    }
+#pragma unroll 8
+    for (int g = 0; g < G; ++g) w += part[g].weight[b];
+    sh.before[b] = w;
+    sh.places[b] = c;
+  }
+  uint64_t near = 0;
+  if (p.use_m())
+    for (int g = 0; g < G; ++g) near += part[g].near;
+  __syncthreads();
+  pick(a, sh, r, p, scale_of(p, m), near);
+}
+
+// How long rows are cut up.
+struct Plan {
+  int64_t group;  // rows per group of launches
+  int G;          // workgroups per row in the first two walks
+  int stretch;    // tokens per workgroup
+};
+
+Plan plan_of(int64_t rows, int64_t vocab) {
+  Plan p;
+  // a group's logits within half of the 256 MB cache
+  const int64_t fit = (int64_t(1) << 27) / (4 * vocab);
+  p.group = rows < fit ? rows : fit;
+  if (p.group > 1024) p.group = 1024;
+  // enough workgroups to fill the compute units twice, each with 4096 tokens or more
+  int64_t G = 512 / p.group;
+  if (G > vocab / 4096) G = vocab / 4096;
+  if (G > 32) G = 32;
+  if (G < 1) G = 1;
+  p.stretch = static_cast<int>(((vocab + G - 1) / G + 3) / 4 * 4);
+  p.G = static_cast<int>((vocab + p.stretch - 1) / p.stretch);
+  return p;
+}
+
+constexpr int64_t kOneLaunch = 16384;  // longest row of the single launch
 
 }  // namespace
 
-uint64_t sample_workspace_bytes(int64_t, int64_t) { return 0; }
+uint64_t sample_workspace_bytes(int64_t rows, int64_t vocab) {
+  if (vocab <= kOneLaunch || rows <= 0) return 0;
+  const Plan p = plan_of(rows, vocab);
+  return static_cast<uint64_t>(p.group) * static_cast<uint64_t>(p.G) * sizeof(Part);
+}
 
-hipError_t launch_sample(const SampleArgs& a, void*, hipStream_t s) {
-  const int64_t cap = int64_t(1) << 20;
-  hipLaunchKernelGGL(sample_kernel, dim3(static_cast<unsigned>(a.rows < cap ? a.rows : cap)), dim3(kThreads), 0,
-                     s, a);
-  return hipGetLastError();
+hipError_t launch_sample(const SampleArgs& a, void* workspace, hipStream_t s) {
+  if (a.vocab <= kOneLaunch) {
+    const int64_t cap = int64_t(1) << 20;
+    hipLaunchKernelGGL(sample_kernel, dim3(static_cast<unsigned>(a.rows < cap ? a.rows : cap)),
+                       dim3(kThreads), 0, s, a);
+    return hipGetLastError();
+  }
+  const Plan p = plan_of(a.rows, a.vocab);
+  Part* parts = static_cast<Part*>(workspace);
+  for (int64_t r0 = 0; r0 < a.rows; r0 += p.group) {
+    SampleArgs g = a;
+    g.rows = a.rows - r0 < p.group ? a.rows - r0 : p.group;
+    g.L = a.L + r0 * a.ldl;
+    g.u = a.u + r0;
+    if (a.temperature) g.temperature = a.temperature + r0;
+    if (a.top_k) g.top_k = a.top_k + r0;
+    if (a.top_p) g.top_p = a.top_p + r0;
+    if (a.min_p) g.min_p = a.min_p + r0;
+    g.token = a.token + r0;
+    if (a.prob) g.prob = a.prob + r0;
+    const dim3 wide(static_cast<unsigned>(g.rows * p.G)), rows(static_cast<unsigned>(g.rows));
+    hipLaunchKernelGGL(sample_top_kernel, wide, dim3(kWeighThreads), 0, s, g, parts, p.G, p.stretch);
+    hipLaunchKernelGGL(sample_weigh_kernel, wide, dim3(kWeighThreads), 0, s, g, parts, p.G,
+                       p.stretch);
+    hipLaunchKernelGGL(sample_pick_kernel, rows, dim3(kThreads), 0, s, g, parts, p.G);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace repops
