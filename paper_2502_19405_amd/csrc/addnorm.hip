@@ -58,18 +58,37 @@ __device__ __forceinline__ void store_sums(const AddNormArgs& a, int64_t row, in
   }
 }
 
+// gamma of the lane's columns: read with the row where a lane holds few values, at its
+// use otherwise (there are not the registers).
+template <int T>
+struct Gamma {
+  static constexpr bool kPre = T <= 16;
+  float v[kPre ? T : 1];
+  __device__ __forceinline__ void load(const AddNormArgs& a, int64_t j0) {
+    if constexpr (kPre) {
+#pragma unroll
+      for (int t = 0; t < T; ++t) {
+        const int64_t j = j0 + kWave * t;
+        v[t] = 0.0f;
+        if (a.gamma && j < a.cols) v[t] = a.gamma[j];
+      }
+    }
+  }
+  __device__ __forceinline__ float at(const AddNormArgs& a, int64_t j, int t) const {
+    if constexpr (kPre) return v[t];
+    else return j < a.cols ? a.gamma[j] : 0.0f;
+  }
+};
+
 // v becomes y, and is stored where Y is wanted.
 template <int T>
 __device__ __forceinline__ void finish_rows(const AddNormArgs& a, int64_t row, int64_t j0,
-                                            float rstd, float (&v)[T]) {
+                                            float rstd, const Gamma<T>& gamma, float (&v)[T]) {
 #pragma unroll
   for (int t = 0; t < T; ++t) v[t] = v[t] * rstd;
   if (a.gamma) {
 #pragma unroll
-    for (int t = 0; t < T; ++t) {
-      const int64_t j = j0 + kWave * t;
-      if (j < a.cols) v[t] = v[t] * a.gamma[j];
-    }
+    for (int t = 0; t < T; ++t) v[t] = v[t] * gamma.at(a, j0 + kWave * t, t);
   }
   if (a.Y) {
     float* y = a.Y + row * a.ldy;
@@ -93,34 +112,61 @@ __device__ __forceinline__ uint32_t lane_max(const AddNormArgs& a, int64_t j0,
   return m;
 }
 
+// The codes of a wave's columns c0 .. c0 + 64 T - 1.  The row order gives a lane
+// every 64th column: the codes turn through LDS (buf: 64 T bytes of the wave's own) so
+// that a lane stores 4 neighbouring ones (stored byte by byte from where they are,
+// 4096 x 4096 took 87 us).
 template <int T>
-__device__ __forceinline__ void store_codes(const AddNormArgs& a, int64_t row, int64_t j0,
-                                            float scale, const float (&v)[T]) {
-  int8_t* q = a.Q + row * a.ldq;
+__device__ __forceinline__ void store_codes(const AddNormArgs& a, int64_t row, int64_t c0, int lane,
+                                            float scale, const float (&v)[T], int8_t* buf) {
+  int code[T];
+  quant_codes<T>(v, scale, code);
+  int8_t* q = a.Q + row * a.ldq + c0;
+  const int64_t left = a.cols - c0;
+  if constexpr (T < 4) {
 #pragma unroll
-  for (int t = 0; t < T; ++t) {
-    const int64_t j = j0 + kWave * t;
-    if (j < a.cols) q[j] = static_cast<int8_t>(quant_code(v[t], scale));
+    for (int t = 0; t < T; ++t)
+      if (lane + kWave * t < left) q[lane + kWave * t] = static_cast<int8_t>(code[t]);
+  } else {
+#pragma unroll
+    for (int t = 0; t < T; ++t) buf[lane + kWave * t] = static_cast<int8_t>(code[t]);
+    // (one wave's LDS operations complete in order)
+#pragma unroll
+    for (int w = 0; w < T / 4; ++w) {
+      const int at = (lane + kWave * w) * 4;
+      const uint32_t four = *reinterpret_cast<const uint32_t*>(buf + at);
+      if (at + 4 <= left) {
+        __builtin_memcpy(q + at, &four, 4);  // any alignment
+      } else {
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+          if (at + k < left) q[at + k] = static_cast<int8_t>(four >> (8 * k));
+      }
+    }
   }
 }
 
 template <int T>
 __global__ __launch_bounds__(512) void addnorm_wave_kernel(AddNormArgs a, int wpb) {
+  __shared__ alignas(4) int8_t codes[8][T * kWave];
   const int lane = threadIdx.x & (kWave - 1);
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * wpb + wave_id();
+  const int w = wave_id();
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * wpb + w;
   if (row >= a.rows) return;
   float v[T];
+  Gamma<T> gamma;
   load_sums<T>(a, row, lane, v);
+  gamma.load(a, lane);
   if (a.S) store_sums<T>(a, row, lane, v);
   float q = 0.0f;
 #pragma unroll
   for (int t = 0; t < T; ++t) q = __builtin_fmaf(v[t], v[t], q);  // past the row: fma(0, 0, q) = q
   const float ms = wave_tree_sum(q) / static_cast<float>(a.cols);
   const float rstd = 1.0f / __builtin_sqrtf(ms + a.eps);
-  finish_rows<T>(a, row, lane, rstd, v);
+  finish_rows<T>(a, row, lane, rstd, gamma, v);
   if (a.Q) {
     const float scale = quant_scale(wave_max_bits(lane_max<T>(a, lane, v)));
-    store_codes<T>(a, row, lane, scale, v);
+    store_codes<T>(a, row, 0, lane, scale, v, codes[w]);
     if (lane == 0) a.scale[row] = scale;
   }
   if (lane == 0 && a.rstd_out) a.rstd_out[row] = rstd;
@@ -133,13 +179,16 @@ template <int T>
 __global__ __launch_bounds__(512) void addnorm_split_kernel(AddNormArgs a) {
   __shared__ float chain[kWave];
   __shared__ uint32_t wave_top[8];
+  __shared__ alignas(4) int8_t codes[8][T * kWave];
   const int lane = threadIdx.x & (kWave - 1);
   const int w = wave_id();
   const int S = static_cast<int>(blockDim.x >> 6);
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const int64_t j0 = lane + int64_t(kWave) * T * w;
+    const int64_t c0 = int64_t(kWave) * T * w, j0 = c0 + lane;
     float v[T];
+    Gamma<T> gamma;
     load_sums<T>(a, row, j0, v);
+    gamma.load(a, j0);
     if (a.S) store_sums<T>(a, row, j0, v);
     const float q = chain_across_waves(chain, lane, w, S, [&](float c) {
 #pragma unroll
@@ -148,7 +197,7 @@ __global__ __launch_bounds__(512) void addnorm_split_kernel(AddNormArgs a) {
     });
     const float ms = wave_tree_sum(q) / static_cast<float>(a.cols);
     const float rstd = 1.0f / __builtin_sqrtf(ms + a.eps);
-    finish_rows<T>(a, row, j0, rstd, v);
+    finish_rows<T>(a, row, j0, rstd, gamma, v);
     if (a.Q) {
       const uint32_t top = wave_max_bits(lane_max<T>(a, j0, v));
       if (lane == 0) wave_top[w] = top;
@@ -156,7 +205,7 @@ __global__ __launch_bounds__(512) void addnorm_split_kernel(AddNormArgs a) {
       uint32_t m = 0;
       for (int k = 0; k < S; ++k) m = wave_top[k] > m ? wave_top[k] : m;
       const float scale = quant_scale(m);
-      store_codes<T>(a, row, j0, scale, v);
+      store_codes<T>(a, row, c0, lane, scale, v, codes[w]);
       if (w == 0 && lane == 0) a.scale[row] = scale;
     }
     if (w == 0 && lane == 0 && a.rstd_out) a.rstd_out[row] = rstd;
@@ -207,29 +256,90 @@ __global__ __launch_bounds__(64) void addnorm_generic_kernel(AddNormArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// 8-bit codes of rows: one workgroup per row, the row read for its maximum and
-// again for its codes.
+// 8-bit codes of rows.  The largest magnitude is the same in any order, so a thread
+// takes 4 neighbouring columns at a time: 16 bytes read, 4 stored.  Rows of up to 16
+// values a thread stay in registers between the maximum and the codes.
 // ---------------------------------------------------------------------------
 
-__global__ __launch_bounds__(256) void quantize_kernel(QuantArgs a) {
-  __shared__ uint32_t wave_top[4];
-  const int tid = threadIdx.x;
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+// The 4 values from column j on, +0 past the row.
+__device__ __forceinline__ void load_four(const float* x, int64_t j, int64_t cols, float (&v)[4]) {
+  if (j + 4 <= cols) {
+    __builtin_memcpy(v, x + j, 16);  // any alignment
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[k] = 0.0f;
+      if (j + k < cols) v[k] = x[j + k];
+    }
+  }
+}
+
+__device__ __forceinline__ void store_four(int8_t* q, int64_t j, int64_t cols, const int (&c)[4]) {
+  const uint32_t four = (c[0] & 255) | (c[1] & 255) << 8 | (c[2] & 255) << 16 | c[3] << 24;
+  if (j + 4 <= cols) {
+    __builtin_memcpy(q + j, &four, 4);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (j + k < cols) q[j + k] = static_cast<int8_t>(four >> (8 * k));
+  }
+}
+
+// NT threads a row (64: a wave a row, four to a workgroup), rows of at most 16 NT
+// columns; LOOP: any width, the row read twice.
+template <int NT, bool LOOP>
+__global__ __launch_bounds__(NT < 256 ? 256 : NT) void quantize_kernel(QuantArgs a) {
+  constexpr int V = 4;  // groups of 4 held per thread
+  constexpr int kRows = NT < 256 ? 256 / NT : 1;
+  __shared__ uint32_t wave_top[NT / 64];
+  const int tid = threadIdx.x % NT;
+  for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * kRows; r0 < a.rows;
+       r0 += static_cast<int64_t>(gridDim.x) * kRows) {
+    const int64_t row = r0 + threadIdx.x / NT;
+    if (row >= a.rows) break;  // (only where a wave has its own row)
     const float* x = a.X + row * a.ldx;
     int8_t* q = a.Q + row * a.ldq;
+    float v[V][4];
     uint32_t m = 0;
-    for (int64_t j = tid; j < a.cols; j += 256) {
-      const uint32_t b = mag_bits(x[j]);
-      m = b > m ? b : m;
+    auto top = [&](const float (&f)[4]) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) m = mag_bits(f[k]) > m ? mag_bits(f[k]) : m;
+    };
+    if constexpr (LOOP) {
+      for (int64_t j = tid * 4; j < a.cols; j += NT * 4) {
+        load_four(x, j, a.cols, v[0]);
+        top(v[0]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) load_four(x, (tid + i * NT) * 4, a.cols, v[i]);
+#pragma unroll
+      for (int i = 0; i < V; ++i) top(v[i]);
     }
     m = wave_max_bits(m);
-    if ((tid & 63) == 0) wave_top[tid >> 6] = m;
-    __syncthreads();
-    for (int k = 0; k < 4; ++k) m = wave_top[k] > m ? wave_top[k] : m;
+    if constexpr (NT > 64) {
+      if ((tid & 63) == 0) wave_top[tid >> 6] = m;
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < NT / 64; ++k) m = wave_top[k] > m ? wave_top[k] : m;
+    }
     const float scale = quant_scale(m);
-    for (int64_t j = tid; j < a.cols; j += 256) q[j] = static_cast<int8_t>(quant_code(x[j], scale));
+    int c[4];
+    if constexpr (LOOP) {
+      for (int64_t j = tid * 4; j < a.cols; j += NT * 4) {
+        load_four(x, j, a.cols, v[0]);
+        quant_codes<4>(v[0], scale, c);
+        store_four(q, j, a.cols, c);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        quant_codes<4>(v[i], scale, c);
+        if ((tid + i * NT) * 4 < a.cols) store_four(q, (tid + i * NT) * 4, a.cols, c);
+      }
+    }
     if (tid == 0) a.scale[row] = scale;
-    __syncthreads();
+    if constexpr (NT > 64) __syncthreads();  // the maxima are read before the next row's
   }
 }
 
@@ -246,7 +356,7 @@ WaveKernel pick_wave(int64_t cols) {
 }
 
 unsigned row_blocks(int64_t rows) {
-  const int64_t cap = int64_t(1) << 22;  // workgroups loop over the rows beyond
+  const int64_t cap = int64_t(1) << 21;  // workgroups loop over the rows beyond
   return static_cast<unsigned>(rows < cap ? rows : cap);
 }
 
@@ -279,7 +389,15 @@ hipError_t launch_addnorm_generic(const AddNormArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_quantize(const QuantArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL(quantize_kernel, dim3(row_blocks(a.rows)), dim3(256), 0, s, a);
+  if (a.cols <= 16 * 64)
+    hipLaunchKernelGGL((quantize_kernel<64, false>), dim3(row_blocks((a.rows + 3) / 4)), dim3(256),
+                       0, s, a);
+  else if (a.cols <= 16 * 256)
+    hipLaunchKernelGGL((quantize_kernel<256, false>), dim3(row_blocks(a.rows)), dim3(256), 0, s, a);
+  else if (a.cols <= 16 * 1024)
+    hipLaunchKernelGGL((quantize_kernel<1024, false>), dim3(row_blocks(a.rows)), dim3(1024), 0, s, a);
+  else
+    hipLaunchKernelGGL((quantize_kernel<1024, true>), dim3(row_blocks(a.rows)), dim3(1024), 0, s, a);
   return hipGetLastError();
 }
 
