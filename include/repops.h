@@ -670,9 +670,10 @@ repops_status_t repops_gelu_erf_backward(const repops_order_t *order, int64_t n,
  * wanted, the 8-bit codes of its output:
  *     s_j = RN(x_j + r_j) (s = x if R is NULL);
  *     ms, rstd, y_j as repops_rmsnorm_rows computes them from s;
- *     scale = RN(max |y_j| / 127);  q_j = rint(RN(y_j / scale)) (ties to even),
- *     clamped to +-127.  scale = 0 gives codes 0.  A row with a y that is not
- *     finite gets scale NaN and codes 0.
+ *     scale = RN(max |y_j| / 127);  r = RN(1 / (scale * c));
+ *     q_j = rint(RN(y_j * c * r)) (ties to even), clamped to +-127, with c = 1, or
+ *     2^120 for a scale below 2^-100.  scale = 0 gives codes 0.  A row with a y that
+ *     is not finite gets scale NaN and codes 0.
  *   X, ldx; R, ldr     rows x cols; R may be NULL.
  *   S, lds             NULL or output for the sum.
  *   Y, ldy             NULL or output for y.

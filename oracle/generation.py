@@ -1,8 +1,8 @@
 """CPU oracle of the generation-step operators (TEST INFRASTRUCTURE ONLY).
 
 The residual addition with its norm is one binary32 addition and the norm's
-oracle; the 8-bit codes are numpy's binary32 division and rounding to even (both
-IEEE operations); the 8-bit product is an exact integer product and three rounded
+oracle; the 8-bit codes are numpy's binary32 divisions, products and rounding to even
+(all IEEE operations); the 8-bit product is an exact integer product and three rounded
 multiplications; the drawing of a token is ``sample_ref.c``.  No code is shared
 with the GPU path.
 """
@@ -60,9 +60,10 @@ def quantize_rows(Y):
         top = np.abs(Y).max(axis=1, initial=0.0) if Y.size else np.zeros(len(Y), np.float32)
         top = np.where(np.isfinite(Y).all(axis=1), top, np.float32(np.nan)).astype(np.float32)
         scale = (top / np.float32(127.0)).astype(np.float32)
-        q = np.rint((Y / scale[:, None]).astype(np.float32))
-        q = np.clip(q, -127, 127)
-        q = np.where(scale[:, None] > 0, q, 0)
+        lift = np.where(scale < np.float32(2.0 ** -100), np.float32(2.0 ** 120), np.float32(1.0))
+        r = (np.float32(1.0) / (scale * lift).astype(np.float32)).astype(np.float32)
+        q = np.rint(((Y * lift[:, None]).astype(np.float32) * r[:, None]).astype(np.float32))
+        q = np.where(scale[:, None] > 0, np.clip(q, -127, 127), 0)
     return q.astype(np.int8), scale
 
 

@@ -4,7 +4,7 @@
 // rstd = 1 / sqrt(ms + eps); y = RN(s rstd) gamma: the sequence of
 // repops_rmsnorm_rows on the rounded sum, so y has its bits.  The codes of y
 // (quantize.h) leave in the same pass: with a scale per row the values stay in
-// registers between the maximum and the division.
+// registers between the maximum and the codes.
 //
 // Bound: memory.  8 B read and 4 (S) + 4 (Y) or 1 (codes) B written per
 // element; the sum never goes out and back for the norm to read it.
@@ -119,17 +119,16 @@ __device__ __forceinline__ uint32_t lane_max(const AddNormArgs& a, int64_t j0,
 template <int T>
 __device__ __forceinline__ void store_codes(const AddNormArgs& a, int64_t row, int64_t c0, int lane,
                                             float scale, const float (&v)[T], int8_t* buf) {
-  int code[T];
-  quant_codes<T>(v, scale, code);
+  const Quantizer code(scale);
   int8_t* q = a.Q + row * a.ldq + c0;
   const int64_t left = a.cols - c0;
   if constexpr (T < 4) {
 #pragma unroll
     for (int t = 0; t < T; ++t)
-      if (lane + kWave * t < left) q[lane + kWave * t] = static_cast<int8_t>(code[t]);
+      if (lane + kWave * t < left) q[lane + kWave * t] = static_cast<int8_t>(code(v[t]));
   } else {
 #pragma unroll
-    for (int t = 0; t < T; ++t) buf[lane + kWave * t] = static_cast<int8_t>(code[t]);
+    for (int t = 0; t < T; ++t) buf[lane + kWave * t] = static_cast<int8_t>(code(v[t]));
     // (one wave's LDS operations complete in order)
 #pragma unroll
     for (int w = 0; w < T / 4; ++w) {
@@ -243,12 +242,13 @@ __global__ __launch_bounds__(64) void addnorm_generic_kernel(AddNormArgs a) {
       scale = quant_scale(wave_max_bits(m));
       if (lane == 0) a.scale[row] = scale;
     }
+    const Quantizer code(scale);
     for (int64_t j = lane; j < a.cols; j += kWave) {
       const float s = sum_at(j);
       const float y = y_of(s, j);
       if (a.S) st_stream(a.S + row * a.lds + j, s);
       if (a.Y) st_stream(a.Y + row * a.ldy + j, y);
-      if (a.Q) a.Q[row * a.ldq + j] = static_cast<int8_t>(quant_code(y, scale));
+      if (a.Q) a.Q[row * a.ldq + j] = static_cast<int8_t>(code(y));
     }
     if (lane == 0 && a.rstd_out) a.rstd_out[row] = rstd;
     __syncthreads();
@@ -324,17 +324,22 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void quantize_kernel(QuantArgs
       for (int k = 0; k < NT / 64; ++k) m = wave_top[k] > m ? wave_top[k] : m;
     }
     const float scale = quant_scale(m);
+    const Quantizer code(scale);
     int c[4];
+    auto codes = [&](const float (&f)[4]) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) c[k] = code(f[k]);
+    };
     if constexpr (LOOP) {
       for (int64_t j = tid * 4; j < a.cols; j += NT * 4) {
         load_four(x, j, a.cols, v[0]);
-        quant_codes<4>(v[0], scale, c);
+        codes(v[0]);
         store_four(q, j, a.cols, c);
       }
     } else {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        quant_codes<4>(v[i], scale, c);
+        codes(v[i]);
         if ((tid + i * NT) * 4 < a.cols) store_four(q, (tid + i * NT) * 4, a.cols, c);
       }
     }

@@ -1,7 +1,8 @@
 // Symmetric 8-bit codes of a row: scale = RN(max |v| / 127), code =
-// rint(RN(v / scale)) within +-127.  The maximum is taken over the bit patterns
-// of |v| as integers: exact in any order, and a NaN (whose pattern is above
-// infinity's) is never lost.
+// rint(RN(v RN(1 / scale))) within +-127, the reciprocal taken once a row (a division
+// a value would be most of the kernels' instructions).  The maximum is taken over the
+// bit patterns of |v| as integers: exact in any order, and a NaN (whose pattern is
+// above infinity's) is never lost.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -35,37 +36,19 @@ __device__ __forceinline__ float quant_scale(uint32_t amax) {
   return amax >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : __uint_as_float(amax) / 127.0f;
 }
 
-// One code.  scale > 0 and finite: v / scale is within 127 but for the rounding of
-// a subnormal scale, which the clamp bounds.  scale +0 (a row of zeros, or of
-// values whose scale underflows) and NaN give code 0.
-__device__ __forceinline__ int quant_code(float v, float scale) {
-  if (!(scale > 0.0f)) return 0;
-  float q = __builtin_rintf(v / scale);
-  q = q > 127.0f ? 127.0f : q;
-  q = q < -127.0f ? -127.0f : q;
-  return static_cast<int>(q);
-}
-
-// The codes of N values, mostly without their division.  With r = RN(1 / scale)
-// from a scale of 2^-100 or more, v r is within 127 * 3 * 2^-24 < 2^-15 of v / scale:
-// unless it lies that near to halfway between two integers (one value in 16000),
-// both round to the same one.  The rest of the wave's values then divide.
-template <int N>
-__device__ __forceinline__ void quant_codes(const float (&v)[N], float scale, int (&code)[N]) {
-  const bool plain = scale >= 0x1p-100f;  // not of a NaN
-  const float r = 1.0f / scale;
-  bool near = !plain;
-#pragma unroll
-  for (int t = 0; t < N; ++t) {
-    const float x = v[t] * r;
-    const float q = __builtin_rintf(x);
-    near |= __builtin_fabsf(x - q) > 0.5f - 0x1p-15f;
-    code[t] = static_cast<int>(q);
+// The codes of a row's values.  A scale below 2^-100, whose reciprocal might overflow,
+// is taken 2^120 times with the values (exact).  The clamp bounds what the rounding of
+// a subnormal scale leaves.  Scale +0 (a row of zeros, or of values whose scale
+// underflows) and NaN give codes 0.
+struct Quantizer {
+  float lift, r;
+  bool live;
+  __device__ __forceinline__ explicit Quantizer(float scale)
+      : lift(scale < 0x1p-100f ? 0x1p120f : 1.0f), r(1.0f / (scale * lift)), live(scale > 0.0f) {}
+  __device__ __forceinline__ int operator()(float v) const {
+    const float q = __builtin_rintf(v * lift * r);
+    return live ? static_cast<int>(q > 127.0f ? 127.0f : q < -127.0f ? -127.0f : q) : 0;
   }
-  if (__any(near)) {
-#pragma unroll
-    for (int t = 0; t < N; ++t) code[t] = quant_code(v[t], scale);
-  }
-}
+};
 
 }  // namespace repops

@@ -252,8 +252,8 @@ def test_quantize_rows(rp, cols):
 
 
 def test_quantize_rows_errs_by_half_a_step(rp):
-    """RN(y / scale) is at most 127 (1 + 2 U): off by less than 2^-16, so a code is
-    within half a step and 2^-16 of one of y / scale."""
+    """RN(y RN(1 / scale)) is within 127 * 2 U < 2^-16 of y / scale, so a code is
+    within half a step and 2^-16."""
     g = inputs.rng(995)
     X = inputs.normal(g, (50, 777))
     announce("quantize_rows half a step")
