@@ -21,41 +21,47 @@
 namespace repops {
 namespace {
 
-// The columns j0 + 64 t (t < T) of one row: sums into v, all loads issued
-// before any arithmetic, +0 past the row.
-template <int T>
-__device__ __forceinline__ void load_sums(const AddNormArgs& a, int64_t row, int64_t j0,
-                                          float (&v)[T]) {
-  const float* x = a.X + row * a.ldx;
+// N values from column j0 on, 64 apart, +0 past the row: read from the last column
+// there and then dropped.  (Loads under a condition each, which implies the ones before
+// it, became code for every width: 65 KB and 3 KB of spills for 32 values a lane.)
+template <int N>
+__device__ __forceinline__ void load_row(const float* x, int j0, int cols, float (&v)[N]) {
 #pragma unroll
-  for (int t = 0; t < T; ++t) {
-    const int64_t j = j0 + kWave * t;
-    v[t] = 0.0f;
-    if (j < a.cols) v[t] = x[j];
+  for (int t = 0; t < N; ++t) {
+    const int j = j0 + kWave * t;
+    v[t] = x[j < cols ? j : cols - 1];
   }
+#pragma unroll
+  for (int t = 0; t < N; ++t) v[t] = j0 + kWave * t < cols ? v[t] : 0.0f;
+}
+
+// The columns j0 + 64 t (t < T) of one row: sums into v, the loads of many values
+// issued before any arithmetic.
+template <int T>
+__device__ __forceinline__ void load_sums(const AddNormArgs& a, int64_t row, int j0,
+                                          float (&v)[T]) {
+  const int cols = static_cast<int>(a.cols);  // at most 2^24
+  load_row<T>(a.X + row * a.ldx, j0, cols, v);
   if (a.R) {
     const float* r = a.R + row * a.ldr;
-    float rv[T];
+    constexpr int B = T < 16 ? T : 16;  // at a time
 #pragma unroll
-    for (int t = 0; t < T; ++t) {
-      const int64_t j = j0 + kWave * t;
-      rv[t] = 0.0f;
-      if (j < a.cols) rv[t] = r[j];
+    for (int t0 = 0; t0 < T; t0 += B) {
+      float rv[B];
+      load_row<B>(r, j0 + kWave * t0, cols, rv);
+#pragma unroll
+      for (int t = 0; t < B; ++t) v[t0 + t] = v[t0 + t] + rv[t];
     }
-#pragma unroll
-    for (int t = 0; t < T; ++t) v[t] = v[t] + rv[t];
   }
 }
 
 template <int T>
-__device__ __forceinline__ void store_sums(const AddNormArgs& a, int64_t row, int64_t j0,
-                                           const float (&v)[T]) {
-  float* s = a.S + row * a.lds;
+__device__ __forceinline__ void store_row(const AddNormArgs& a, float* s, int j0,
+                                          const float (&v)[T]) {
+  const int cols = static_cast<int>(a.cols);
 #pragma unroll
-  for (int t = 0; t < T; ++t) {
-    const int64_t j = j0 + kWave * t;
-    if (j < a.cols) st_stream(s + j, v[t]);
-  }
+  for (int t = 0; t < T; ++t)
+    if (j0 + kWave * t < cols) st_stream(s + j0 + kWave * t, v[t]);
 }
 
 // gamma of the lane's columns: read with the row where a lane holds few values, at its
@@ -64,49 +70,43 @@ template <int T>
 struct Gamma {
   static constexpr bool kPre = T <= 16;
   float v[kPre ? T : 1];
-  __device__ __forceinline__ void load(const AddNormArgs& a, int64_t j0) {
-    if constexpr (kPre) {
-#pragma unroll
-      for (int t = 0; t < T; ++t) {
-        const int64_t j = j0 + kWave * t;
-        v[t] = 0.0f;
-        if (a.gamma && j < a.cols) v[t] = a.gamma[j];
-      }
-    }
-  }
-  __device__ __forceinline__ float at(const AddNormArgs& a, int64_t j, int t) const {
-    if constexpr (kPre) return v[t];
-    else return j < a.cols ? a.gamma[j] : 0.0f;
+  __device__ __forceinline__ void load(const AddNormArgs& a, int j0) {
+    if constexpr (kPre)
+      if (a.gamma) load_row<T>(a.gamma, j0, static_cast<int>(a.cols), v);
   }
 };
 
 // v becomes y, and is stored where Y is wanted.
 template <int T>
-__device__ __forceinline__ void finish_rows(const AddNormArgs& a, int64_t row, int64_t j0,
-                                            float rstd, const Gamma<T>& gamma, float (&v)[T]) {
+__device__ __forceinline__ void finish_rows(const AddNormArgs& a, int64_t row, int j0, float rstd,
+                                            const Gamma<T>& gamma, float (&v)[T]) {
 #pragma unroll
   for (int t = 0; t < T; ++t) v[t] = v[t] * rstd;
   if (a.gamma) {
+    if constexpr (Gamma<T>::kPre) {
 #pragma unroll
-    for (int t = 0; t < T; ++t) v[t] = v[t] * gamma.at(a, j0 + kWave * t, t);
-  }
-  if (a.Y) {
-    float* y = a.Y + row * a.ldy;
+      for (int t = 0; t < T; ++t) v[t] = v[t] * gamma.v[t];
+    } else {
+      constexpr int B = 16;
 #pragma unroll
-    for (int t = 0; t < T; ++t) {
-      const int64_t j = j0 + kWave * t;
-      if (j < a.cols) st_stream(y + j, v[t]);
+      for (int t0 = 0; t0 < T; t0 += B) {
+        float g[B];
+        load_row<B>(a.gamma, j0 + kWave * t0, static_cast<int>(a.cols), g);
+#pragma unroll
+        for (int t = 0; t < B; ++t) v[t0 + t] = v[t0 + t] * g[t];
+      }
     }
   }
+  if (a.Y) store_row<T>(a, a.Y + row * a.ldy, j0, v);
 }
 
 template <int T>
-__device__ __forceinline__ uint32_t lane_max(const AddNormArgs& a, int64_t j0,
-                                             const float (&v)[T]) {
+__device__ __forceinline__ uint32_t lane_max(const AddNormArgs& a, int j0, const float (&v)[T]) {
+  const int cols = static_cast<int>(a.cols);
   uint32_t m = 0;
 #pragma unroll
   for (int t = 0; t < T; ++t) {
-    const uint32_t b = j0 + kWave * t < a.cols ? mag_bits(v[t]) : 0u;
+    const uint32_t b = j0 + kWave * t < cols ? mag_bits(v[t]) : 0u;
     m = b > m ? b : m;
   }
   return m;
@@ -117,11 +117,11 @@ __device__ __forceinline__ uint32_t lane_max(const AddNormArgs& a, int64_t j0,
 // that a lane stores 4 neighbouring ones (stored byte by byte from where they are,
 // 4096 x 4096 took 87 us).
 template <int T>
-__device__ __forceinline__ void store_codes(const AddNormArgs& a, int64_t row, int64_t c0, int lane,
+__device__ __forceinline__ void store_codes(const AddNormArgs& a, int64_t row, int c0, int lane,
                                             float scale, const float (&v)[T], int8_t* buf) {
   const Quantizer code(scale);
   int8_t* q = a.Q + row * a.ldq + c0;
-  const int64_t left = a.cols - c0;
+  const int left = static_cast<int>(a.cols) - c0;
   if constexpr (T < 4) {
 #pragma unroll
     for (int t = 0; t < T; ++t)
@@ -129,7 +129,7 @@ __device__ __forceinline__ void store_codes(const AddNormArgs& a, int64_t row, i
   } else {
 #pragma unroll
     for (int t = 0; t < T; ++t) buf[lane + kWave * t] = static_cast<int8_t>(code(v[t]));
-    // (one wave's LDS operations complete in order)
+    wave_lds_fence();
 #pragma unroll
     for (int w = 0; w < T / 4; ++w) {
       const int at = (lane + kWave * w) * 4;
@@ -156,7 +156,7 @@ __global__ __launch_bounds__(512) void addnorm_wave_kernel(AddNormArgs a, int wp
   Gamma<T> gamma;
   load_sums<T>(a, row, lane, v);
   gamma.load(a, lane);
-  if (a.S) store_sums<T>(a, row, lane, v);
+  if (a.S) store_row<T>(a, a.S + row * a.lds, lane, v);
   float q = 0.0f;
 #pragma unroll
   for (int t = 0; t < T; ++t) q = __builtin_fmaf(v[t], v[t], q);  // past the row: fma(0, 0, q) = q
@@ -183,12 +183,12 @@ __global__ __launch_bounds__(512) void addnorm_split_kernel(AddNormArgs a) {
   const int w = wave_id();
   const int S = static_cast<int>(blockDim.x >> 6);
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const int64_t c0 = int64_t(kWave) * T * w, j0 = c0 + lane;
+    const int c0 = kWave * T * w, j0 = c0 + lane;
     float v[T];
     Gamma<T> gamma;
     load_sums<T>(a, row, j0, v);
     gamma.load(a, j0);
-    if (a.S) store_sums<T>(a, row, j0, v);
+    if (a.S) store_row<T>(a, a.S + row * a.lds, j0, v);
     const float q = chain_across_waves(chain, lane, w, S, [&](float c) {
 #pragma unroll
       for (int t = 0; t < T; ++t) c = __builtin_fmaf(v[t], v[t], c);  // past the row: c

@@ -15,6 +15,7 @@
 
 #include "generation_internal.h"
 #include "repops_internal.h"
+#include "row_reduce.h"
 
 #pragma clang fp contract(off)
 
@@ -32,11 +33,6 @@ template <int N>
 __device__ __forceinline__ void wait_vmcnt() {
   static_assert(N >= 0 && N < 64, "vmcnt range");
   __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
-}
-
-// Workgroup barrier that leaves global-to-LDS loads in flight.
-__device__ __forceinline__ void lds_barrier() {
-  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
 // An output's scales and bias; the rounded steps in their order.
@@ -178,7 +174,7 @@ struct Q8Tile {
 #pragma unroll
       for (int u = 0; u < PER; ++u) issue(sm, src, u, s, s, wave, last);
     wait_vmcnt<(NS - 1) * PER>();
-    lds_barrier();
+    lds_only_barrier();
     Pack pk[2];
 #pragma unroll
     for (int r = 0; r < RD; ++r) read_one(sm.a[0], sm.b[0], rd, 0, r, pk[0]);
@@ -194,7 +190,7 @@ struct Q8Tile {
           __builtin_amdgcn_sched_barrier(0);
           if (closing && t == 0) {
             wait_vmcnt<(NS - 2) * PER>();
-            lds_barrier();
+            lds_only_barrier();
           }
 #pragma unroll
           for (int r = RD * t / MF; r < RD * (t + 1) / MF; ++r)
@@ -300,7 +296,7 @@ struct Q8Tile {
         for (int j = 0; j < IN; ++j)
           turn[(8 * (r / 4) + 4 * (lane >> 5) + r % 4) * PITCH + 32 * j + (lane & 31)] =
               acc[i][j][r];
-      // (one wave's LDS operations complete in order)
+      wave_lds_fence();
 #pragma unroll
       for (int t = 0; t < 32 / RPS; ++t) {
         const int r = t * RPS + lane / LPR;
@@ -329,6 +325,7 @@ struct Q8Tile {
             if (col + c < g.n) out[c] = v[c];
         }
       }
+      wave_lds_fence();
     }
   }
 };

@@ -104,6 +104,14 @@ __device__ __forceinline__ void lds_only_barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
+// Between LDS writes of some of a wave's lanes and reads by others: the hardware
+// completes one wave's LDS operations in order, the compiler must keep them so.
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // Sum of term(j), j in [0, n), in the descriptor's order.  qs is LDS holding at
 // least 1024 floats.  Every lane returns the sum.
 template <class Term>

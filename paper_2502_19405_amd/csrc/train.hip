@@ -162,24 +162,30 @@ __device__ __forceinline__ void ln_bwd_terms(const RowBwdArgs& a, const float* x
   }
 }
 
-// The ADD forms' values of dS in the columns j0 + 64 t of one row, read ahead of
-// the row's reductions (+0 past the row); nothing otherwise.
+// The ADD forms' values of dS in the columns j0 + 64 t of one row: read ahead of the
+// row's reductions (+0 past the row) but behind the use of gamma, whose registers
+// they take (at the top of the row, 4096 columns need 132 registers: one workgroup per
+// compute unit instead of two), or, for 64 values a lane, at their use.  Nothing
+// otherwise.
 template <int T, bool ADD>
 struct AddRow {
-  float v[ADD ? T : 1];
+  static constexpr bool kPre = ADD && T <= 32;
+  float v[kPre ? T : 1];
+  const float* ds;
   __device__ __forceinline__ void load(const RowBwdArgs& a, int64_t row, int64_t j0) {
-    if constexpr (ADD) {
-      const float* ds = a.dS + row * a.ldds;
+    if constexpr (ADD) ds = a.dS + row * a.ldds + j0;
+    if constexpr (kPre) {
 #pragma unroll
       for (int t = 0; t < T; ++t) {
-        const int64_t j = j0 + kWave * t;
         v[t] = 0.0f;
-        if (j < a.cols) v[t] = ds[j];
+        if (j0 + kWave * t < a.cols) v[t] = ds[kWave * t];
       }
     }
   }
+  // (column j0 + 64 t is within the row)
   __device__ __forceinline__ float operator()(int t, float dx) const {
-    if constexpr (ADD) return dx + v[t];
+    if constexpr (kPre) return dx + v[t];
+    else if constexpr (ADD) return dx + ds[kWave * t];
     else return dx;
   }
 };
@@ -192,10 +198,10 @@ __device__ __forceinline__ void layernorm_bwd_row(const RowBwdArgs& a, int64_t r
   const float* dy = a.dY + row * a.lddy;
   float* dx = a.dX + row * a.lddx;
   const float mean = a.rms ? 0.0f : a.mean[row], rstd = a.rstd[row];
-  AddRow<T, ADD> add;
-  add.load(a, row, lane);
   float tv[T], gv[T];
   ln_bwd_terms<T>(a, x, dy, lane, mean, rstd, tv, gv);
+  AddRow<T, ADD> add;
+  add.load(a, row, lane);
   float q = 0.0f;
 #pragma unroll
   for (int t = 0; t < T; ++t) q = q + gv[t];  // terms past the row are +0 and leave q unchanged
@@ -297,10 +303,10 @@ __global__ __launch_bounds__(512) void layernorm_bwd_split_kernel(RowBwdArgs a) 
     float* dx = a.dX + row * a.lddx;
     const float mean = a.rms ? 0.0f : a.mean[row], rstd = a.rstd[row];
     const int64_t j0 = lane + int64_t(kWave) * T * w;
-    AddRow<T, ADD> add;
-    add.load(a, row, j0);
     float tv[T], gv[T];
     ln_bwd_terms<T>(a, x, dy, j0, mean, rstd, tv, gv);
+    AddRow<T, ADD> add;
+    add.load(a, row, j0);
     float am = 0.0f;
     if (!a.rms) {  // uniform over the workgroup
       const float q = chain_across_waves(chain_g, lane, w, S, [&](float c) {
@@ -712,10 +718,10 @@ __device__ __forceinline__ void layernorm_bwd_rows_grouped(const RowBwdArgs& a, 
     const float* dy = a.dY + rr * a.lddy;
     const float mean = a.rms ? 0.0f : a.mean[rr], rstd = a.rstd[rr];
     const int64_t j0 = lane + int64_t(kWave) * T * h;
-    AddRow<T, ADD> add;
-    add.load(a, rr, j0);
     float tv[T], gv[T];
     ln_bwd_terms<T>(a, x, dy, j0, mean, rstd, tv, gv);
+    AddRow<T, ADD> add;
+    add.load(a, rr, j0);
     float am = 0.0f;
     if (!a.rms) {  // uniform over the workgroup
       const float q = group_chain(chain_g, [&](float c) {
