@@ -12,6 +12,7 @@
 
 #include "generation_internal.h"
 #include "quantize.h"
+#include "row_buffer.h"
 #include "row_reduce.h"
 #include "rows_internal.h"
 #include "stream_store.h"
@@ -21,34 +22,23 @@
 namespace repops {
 namespace {
 
-// N values from column j0 on, 64 apart, +0 past the row: read from the last column
-// there and then dropped.  (Loads under a condition each, which implies the ones before
-// it, became code for every width: 65 KB and 3 KB of spills for 32 values a lane.)
-template <int N>
-__device__ __forceinline__ void load_row(const float* x, int j0, int cols, float (&v)[N]) {
-#pragma unroll
-  for (int t = 0; t < N; ++t) {
-    const int j = j0 + kWave * t;
-    v[t] = x[j < cols ? j : cols - 1];
-  }
-#pragma unroll
-  for (int t = 0; t < N; ++t) v[t] = j0 + kWave * t < cols ? v[t] : 0.0f;
-}
-
-// The columns j0 + 64 t (t < T) of one row: sums into v, the loads of many values
-// issued before any arithmetic.
+// The columns j0 + 64 t (t < T) of one row: sums into v (+0 past the row), the loads of
+// many values issued before any arithmetic.
 template <int T>
 __device__ __forceinline__ void load_sums(const AddNormArgs& a, int64_t row, int j0,
                                           float (&v)[T]) {
   const int cols = static_cast<int>(a.cols);  // at most 2^24
-  load_row<T>(a.X + row * a.ldx, j0, cols, v);
+  const RowBuffer x(a.X + row * a.ldx, cols);
+#pragma unroll
+  for (int t = 0; t < T; ++t) v[t] = x.load(j0 + kWave * t);
   if (a.R) {
-    const float* r = a.R + row * a.ldr;
+    const RowBuffer r(a.R + row * a.ldr, cols);
     constexpr int B = T < 16 ? T : 16;  // at a time
 #pragma unroll
     for (int t0 = 0; t0 < T; t0 += B) {
       float rv[B];
-      load_row<B>(r, j0 + kWave * t0, cols, rv);
+#pragma unroll
+      for (int t = 0; t < B; ++t) rv[t] = r.load(j0 + kWave * (t0 + t));
 #pragma unroll
       for (int t = 0; t < B; ++t) v[t0 + t] = v[t0 + t] + rv[t];
     }
@@ -56,12 +46,11 @@ __device__ __forceinline__ void load_sums(const AddNormArgs& a, int64_t row, int
 }
 
 template <int T>
-__device__ __forceinline__ void store_row(const AddNormArgs& a, float* s, int j0,
+__device__ __forceinline__ void store_row(const AddNormArgs& a, float* p, int j0,
                                           const float (&v)[T]) {
-  const int cols = static_cast<int>(a.cols);
+  const RowBuffer out(p, static_cast<int>(a.cols));
 #pragma unroll
-  for (int t = 0; t < T; ++t)
-    if (j0 + kWave * t < cols) st_stream(s + j0 + kWave * t, v[t]);
+  for (int t = 0; t < T; ++t) out.store(j0 + kWave * t, v[t]);
 }
 
 // gamma of the lane's columns: read with the row where a lane holds few values, at its
@@ -71,8 +60,13 @@ struct Gamma {
   static constexpr bool kPre = T <= 16;
   float v[kPre ? T : 1];
   __device__ __forceinline__ void load(const AddNormArgs& a, int j0) {
-    if constexpr (kPre)
-      if (a.gamma) load_row<T>(a.gamma, j0, static_cast<int>(a.cols), v);
+    if constexpr (kPre) {
+      if (a.gamma) {
+        const RowBuffer g(a.gamma, static_cast<int>(a.cols));
+#pragma unroll
+        for (int t = 0; t < T; ++t) v[t] = g.load(j0 + kWave * t);
+      }
+    }
   }
 };
 
@@ -87,14 +81,9 @@ __device__ __forceinline__ void finish_rows(const AddNormArgs& a, int64_t row, i
 #pragma unroll
       for (int t = 0; t < T; ++t) v[t] = v[t] * gamma.v[t];
     } else {
-      constexpr int B = 16;
+      const RowBuffer g(a.gamma, static_cast<int>(a.cols));
 #pragma unroll
-      for (int t0 = 0; t0 < T; t0 += B) {
-        float g[B];
-        load_row<B>(a.gamma, j0 + kWave * t0, static_cast<int>(a.cols), g);
-#pragma unroll
-        for (int t = 0; t < B; ++t) v[t0 + t] = v[t0 + t] * g[t];
-      }
+      for (int t = 0; t < T; ++t) v[t] = v[t] * g.load(j0 + kWave * t);
     }
   }
   if (a.Y) store_row<T>(a, a.Y + row * a.ldy, j0, v);
