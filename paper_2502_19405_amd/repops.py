@@ -872,64 +872,71 @@ Q8_MAX_K = 131071  # REPOPS_Q8_MAX_K
 _I8, _I32 = torch.int8, torch.int32
 
 
-def _same_device(*tensors):
-    """The library is given addresses: all of a call's tensors must be on one device."""
-    dev = None
-    for t in tensors:
-        if t is not None:
-            if dev is None:
-                dev = t.device
-            elif t.device != dev:
-                raise ValueError(f"tensors on different devices: {dev} and {t.device}")
-
-
-def _typed(t: torch.Tensor, dtype, name: str):
+def _at(t: torch.Tensor, dtype, device: int, name: str) -> int:
+    """Address of a tensor of this type on this device."""
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {str(dtype)[6:]}")
-    if not t.is_cuda:
-        raise TypeError(f"{name} must be a device tensor")
+    if t.get_device() != device or device < 0:
+        if not t.is_cuda:
+            raise TypeError(f"{name} must be a device tensor")
+        raise ValueError(f"{name} is on another device ({t.device})")
     return t.data_ptr()
-
-
-def _row_values(t, name: str, rows: int, dtype=_F32):
-    """Pointer of an optional contiguous [rows] device vector."""
-    if t is None:
-        return None
-    if t.shape != (rows,) or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous [{rows}] tensor")
-    return _typed(t, dtype, name)
 
 
 def _row_major(t: torch.Tensor, name: str):
     """_rows, for matrices that may be empty or one column wide, whose column
     stride says nothing."""
-    if t.dim() == 2 and (t.numel() == 0 or t.shape[1] == 1):
-        rows, cols = t.shape
+    shape = t.shape
+    if len(shape) == 2 and (shape[1] <= 1 or shape[0] == 0):
+        rows, cols = shape
         return rows, cols, max(t.stride(0) if rows > 1 and cols else cols, 1)
     return _rows(t, name)
 
 
-def _shaped(t: torch.Tensor, rows: int, cols: int, name: str) -> int:
-    """Row stride of a [rows, cols] matrix."""
-    if t.shape != (rows, cols):
-        raise ValueError(f"{name} must be [{rows}, {cols}] (got {list(t.shape)})")
-    return _row_major(t, name)[2]
+def _matrix(t, shape, dtype, device: int, name: str):
+    """(address, row stride) of an optional matrix of this shape."""
+    if t is None:
+        return None, 0
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)} (got {list(t.shape)})")
+    return _at(t, dtype, device, name), _row_major(t, name)[2]
 
 
-def _add_rmsnorm(X, R, gamma, eps, order, launch, S, Y, Q, scale, rstd_out):
-    rows, cols, ldx = _row_major(X, "X")
-    _same_device(X, R, gamma, S, Y, Q, scale, rstd_out)
-    opt = lambda t, name: (None, 0) if t is None else (  # noqa: E731
-        _dev(t, name), _shaped(t, rows, cols, name))
-    pr, ldr = opt(R, "R")
-    ps, lds = opt(S, "sum_out")
-    py, ldy = opt(Y, "out")
-    pq, ldq = (None, 0) if Q is None else (_typed(Q, _I8, "q_out"), _shaped(Q, rows, cols, "q_out"))
-    rc = (_lib or load()).repops_add_rmsnorm_rows(
-        _ord(order), rows, cols, _dev(X, "X"), ldx, pr, ldr, _vec(gamma, "gamma", cols), float(eps),
-        ps, lds, py, ldy, pq, ldq, _row_values(scale, "scale_out", rows),
-        _row_values(rstd_out, "rstd_out", rows), _launch(launch), _stream(X))
-    _check(rc, "repops_add_rmsnorm_rows")
+def _vector(t, size: int, dtype, device: int, name: str):
+    """Address of an optional contiguous vector."""
+    if t is None:
+        return None
+    if t.shape != (size,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous [{size}] tensor")
+    return _at(t, dtype, device, name)
+
+
+def _call(fn, device: int, *args):
+    """A library call on this device's current stream, with the device current: the
+    library launches on the current one."""
+    if _current_device() == device:
+        rc = fn(*args, _raw_stream(device))
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, _raw_stream(device))
+    if rc != OK:
+        raise RepopsError(rc, fn.__name__)
+
+
+def _current_device() -> int:
+    return torch._C._cuda_getDevice()
+
+
+def _add_rmsnorm(X, ldx, device, R, gamma, eps, order, launch, S, Y, Q, scale, rstd_out):
+    shape = X.shape
+    rows, cols = shape
+    _call((_lib or load()).repops_add_rmsnorm_rows, device, _ord(order), rows, cols,
+          _at(X, _F32, device, "X"), ldx, *_matrix(R, shape, _F32, device, "R"),
+          _vector(gamma, cols, _F32, device, "gamma"), eps,
+          *_matrix(S, shape, _F32, device, "sum_out"), *_matrix(Y, shape, _F32, device, "out"),
+          *_matrix(Q, shape, _I8, device, "q_out"),
+          _vector(scale, rows, _F32, device, "scale_out"),
+          _vector(rstd_out, rows, _F32, device, "rstd_out"), _launch(launch))
 
 
 def add_rmsnorm_rows(X: torch.Tensor, R: torch.Tensor | None = None,
@@ -940,11 +947,13 @@ def add_rmsnorm_rows(X: torch.Tensor, R: torch.Tensor | None = None,
     """(S, Y) with S = X + R and Y = rmsnorm_rows(S, gamma, eps) from one pass.
     R None: Y is the norm of X, and S is X itself unless sum_out is given.  sum_out
     and out may each be X or R."""
+    ldx = _row_major(X, "X")[2]
     if sum_out is None and R is not None:
-        sum_out = torch.empty_like(X, memory_format=torch.contiguous_format)
+        sum_out = X.new_empty(X.shape)
     if out is None:
-        out = torch.empty_like(X, memory_format=torch.contiguous_format)
-    _add_rmsnorm(X, R, gamma, eps, order, launch, sum_out, out, None, None, rstd_out)
+        out = X.new_empty(X.shape)
+    _add_rmsnorm(X, ldx, X.get_device(), R, gamma, eps, order, launch, sum_out, out, None, None,
+                 rstd_out)
     return X if sum_out is None else sum_out, out
 
 
@@ -958,13 +967,15 @@ def add_rmsnorm_quantize_rows(X: torch.Tensor, R: torch.Tensor | None = None,
                               rstd_out: torch.Tensor | None = None):
     """(S, Q, scale): S as add_rmsnorm_rows gives it, and the codes (int8) and
     scales of the Y it gives, which is written only if out is passed."""
+    rows, _, ldx = _row_major(X, "X")
     if sum_out is None and R is not None:
-        sum_out = torch.empty_like(X, memory_format=torch.contiguous_format)
+        sum_out = X.new_empty(X.shape)
     if q_out is None:
-        q_out = torch.empty(X.shape, dtype=_I8, device=X.device)
+        q_out = X.new_empty(X.shape, dtype=_I8)
     if scale_out is None:
-        scale_out = torch.empty(X.shape[:1], dtype=_F32, device=X.device)
-    _add_rmsnorm(X, R, gamma, eps, order, launch, sum_out, out, q_out, scale_out, rstd_out)
+        scale_out = X.new_empty(rows)
+    _add_rmsnorm(X, ldx, X.get_device(), R, gamma, eps, order, launch, sum_out, out, q_out,
+                 scale_out, rstd_out)
     return X if sum_out is None else sum_out, q_out, scale_out
 
 
@@ -979,30 +990,32 @@ def add_rmsnorm_backward_rows(S: torch.Tensor, dY: torch.Tensor, rstd: torch.Ten
     X and of R.  dS is the gradient that reaches S by its other uses; dx_out may be
     S, dY or dS.  Entries not requested are None."""
     rows, cols, lds = _row_major(S, "S")
-    lddy = _shaped(dY, rows, cols, "dY")
-    _same_device(S, dY, rstd, gamma, dS, dx_out, dgamma_out, workspace)
-    pds, ldds = (None, 0) if dS is None else (_dev(dS, "dS"), _shaped(dS, rows, cols, "dS"))
+    shape, device = S.shape, S.get_device()
     dx = dgamma = None
-    lddx = cols
-    if need_dx:
-        dx = dx_out if dx_out is not None else torch.empty_like(S, memory_format=torch.contiguous_format)
-        lddx = _shaped(dx, rows, cols, "dx_out")
     wptr, wbytes = None, 0
+    if need_dx:
+        dx = dx_out if dx_out is not None else S.new_empty(shape)
     if need_dgamma:
-        dgamma = dgamma_out if dgamma_out is not None else torch.empty(cols, dtype=_F32,
-                                                                       device=S.device)
+        dgamma = dgamma_out if dgamma_out is not None else S.new_empty(cols)
         if workspace is None:
             need = rmsnorm_backward_workspace(rows, cols, order)
             if need:
-                workspace = torch.empty(need // 4, dtype=_F32, device=S.device)
-        wptr, wbytes = _workspace(workspace)
-    rc = load().repops_add_rmsnorm_backward_rows(
-        _ord(order), rows, cols, _dev(S, "S"), lds, _dev(dY, "dY"), lddy, pds, ldds,
-        _row_values(rstd, "rstd", rows), _vec(gamma, "gamma", cols),
-        None if dx is None else _dev(dx, "dx_out"), lddx, _vec(dgamma, "dgamma_out", cols), wptr,
-        wbytes, _launch(launch), _stream(S))
-    _check(rc, "repops_add_rmsnorm_backward_rows")
+                workspace = S.new_empty(need // 4)
+        wptr, wbytes = _space(workspace, device)
+    _call((_lib or load()).repops_add_rmsnorm_backward_rows, device, _ord(order), rows, cols,
+          _at(S, _F32, device, "S"), lds, *_matrix(dY, shape, _F32, device, "dY"),
+          *_matrix(dS, shape, _F32, device, "dS"), _vector(rstd, rows, _F32, device, "rstd"),
+          _vector(gamma, cols, _F32, device, "gamma"),
+          *_matrix(dx, shape, _F32, device, "dx_out"),
+          _vector(dgamma, cols, _F32, device, "dgamma_out"), wptr, wbytes, _launch(launch))
     return dx, dgamma
+
+
+def _space(workspace, device: int):
+    """_workspace, on this device."""
+    if workspace is not None and workspace.get_device() != device:
+        raise ValueError(f"workspace is on another device ({workspace.device})")
+    return _workspace(workspace)
 
 
 def quantize_rows(X: torch.Tensor, q_out: torch.Tensor | None = None,
@@ -1010,15 +1023,14 @@ def quantize_rows(X: torch.Tensor, q_out: torch.Tensor | None = None,
     """(Q, scale): 8-bit codes of X [rows, cols] with a scale per row, X near
     Q * scale[:, None]."""
     rows, cols, ldx = _row_major(X, "X")
+    device = X.get_device()
     if q_out is None:
-        q_out = torch.empty(X.shape, dtype=_I8, device=X.device)
+        q_out = X.new_empty(X.shape, dtype=_I8)
     if scale_out is None:
-        scale_out = torch.empty(rows, dtype=_F32, device=X.device)
-    _same_device(X, q_out, scale_out)
-    ldq = _shaped(q_out, rows, cols, "q_out")
-    rc = load().repops_quantize_rows(rows, cols, _dev(X, "X"), ldx, _typed(q_out, _I8, "q_out"), ldq,
-                                     _row_values(scale_out, "scale_out", rows), None, _stream(X))
-    _check(rc, "repops_quantize_rows")
+        scale_out = X.new_empty(rows)
+    _call((_lib or load()).repops_quantize_rows, device, rows, cols, _at(X, _F32, device, "X"), ldx,
+          *_matrix(q_out, X.shape, _I8, device, "q_out"),
+          _vector(scale_out, rows, _F32, device, "scale_out"), None)
     return q_out, scale_out
 
 
@@ -1030,15 +1042,13 @@ def matmul_q8(A: torch.Tensor, a_scale: torch.Tensor, B: torch.Tensor, b_scale: 
     n, k2, ldb = _row_major(B, "B")
     if k != k2:
         raise ValueError(f"inner dimensions differ: {k} vs {k2}")
+    device = A.get_device()
     if out is None:
-        out = torch.empty((m, n), dtype=_F32, device=A.device)
-    _same_device(A, a_scale, B, b_scale, bias, out)
-    ldc = _shaped(out, m, n, "out")
-    rc = (_lib or load()).repops_matmul_q8(
-        m, n, k, _typed(A, _I8, "A"), lda, _row_values(a_scale, "a_scale", m), _typed(B, _I8, "B"),
-        ldb, _row_values(b_scale, "b_scale", n), _row_values(bias, "bias", n), _dev(out, "out"), ldc,
-        None, _stream(out))
-    _check(rc, "repops_matmul_q8")
+        out = A.new_empty((m, n), dtype=_F32)
+    _call((_lib or load()).repops_matmul_q8, device, m, n, k, _at(A, _I8, device, "A"), lda,
+          _vector(a_scale, m, _F32, device, "a_scale"), _at(B, _I8, device, "B"), ldb,
+          _vector(b_scale, n, _F32, device, "b_scale"), _vector(bias, n, _F32, device, "bias"),
+          *_matrix(out, (m, n), _F32, device, "out"), None)
     return out
 
 
@@ -1060,23 +1070,22 @@ def sample_rows(logits: torch.Tensor, u: torch.Tensor, temperature: torch.Tensor
     None for temperature 1 or a filter that is off; temperature 0 takes the likeliest
     token.  A row without a token gives -1."""
     rows, vocab, ldl = _row_major(logits, "logits")
+    device = logits.get_device()
     if token_out is None:
-        token_out = torch.empty(rows, dtype=_I32, device=logits.device)
+        token_out = logits.new_empty(rows, dtype=_I32)
     if prob_out is None:
-        prob_out = torch.empty(rows, dtype=_F32, device=logits.device)
+        prob_out = logits.new_empty(rows)
     if workspace is None:
         need = sample_workspace(rows, vocab)
         if need:
-            workspace = torch.empty(need // 8, dtype=torch.int64, device=logits.device)
-    _same_device(logits, u, temperature, top_k, top_p, min_p, token_out, prob_out, workspace)
-    wptr, wbytes = _workspace(workspace)
-    rc = (_lib or load()).repops_sample_rows(
-        rows, vocab, _dev(logits, "logits"), ldl, _row_values(u, "u", rows),
-        _row_values(temperature, "temperature", rows), _row_values(top_k, "top_k", rows, _I32),
-        _row_values(top_p, "top_p", rows), _row_values(min_p, "min_p", rows),
-        _row_values(token_out, "token_out", rows, _I32), _row_values(prob_out, "prob_out", rows),
-        wptr, wbytes, None, _stream(logits))
-    _check(rc, "repops_sample_rows")
+            workspace = logits.new_empty(need // 8, dtype=torch.int64)
+    _call((_lib or load()).repops_sample_rows, device, rows, vocab,
+          _at(logits, _F32, device, "logits"), ldl, _vector(u, rows, _F32, device, "u"),
+          _vector(temperature, rows, _F32, device, "temperature"),
+          _vector(top_k, rows, _I32, device, "top_k"), _vector(top_p, rows, _F32, device, "top_p"),
+          _vector(min_p, rows, _F32, device, "min_p"),
+          _vector(token_out, rows, _I32, device, "token_out"),
+          _vector(prob_out, rows, _F32, device, "prob_out"), *_space(workspace, device), None)
     return token_out, prob_out
 
 
