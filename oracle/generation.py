@@ -105,3 +105,29 @@ def sample_rows(L, u, temperature=None, top_k=None, top_p=None, min_p=None, lib=
                                        ctypes.byref(p))
         probs[r] = p.value
     return tokens, probs
+
+
+def feed_forward_q8(X, R, gamma, gate, up, down, eps=1e-5):
+    """llama_feed_forward_q8's values by name."""
+    S, N, _ = add_rmsnorm_rows(X, R, gamma, eps)
+    Q, scale = quantize_rows(N)
+    G, U = matmul_q8(Q, scale, *gate), matmul_q8(Q, scale, *up)
+    H = oracle.swiglu(G, U)
+    HQ, h_scale = quantize_rows(H)
+    return {"S": S, "Q": Q, "scale": scale, "G": G, "U": U, "H": H, "HQ": HQ, "h_scale": h_scale,
+            "D": matmul_q8(HQ, h_scale, *down)}
+
+
+def next_token(X, R, gamma, head, u, eps=1e-5, **filters):
+    """llama_next_token's values by name."""
+    Q, scale = quantize_rows(add_rmsnorm_rows(X, R, gamma, eps)[1])
+    logits = matmul_q8(Q, scale, *head)
+    token, prob = sample_rows(logits, u, **filters)
+    return {"Q": Q, "scale": scale, "logits": logits, "token": token, "prob": prob}
+
+
+def norm_linear(X, R, gamma, W, dY, dS=None, eps=1e-5):
+    """(S, Y, dX, dgamma, dW) of norm_linear_forward and its backward."""
+    S, N, rstd = add_rmsnorm_rows(X, R, gamma, eps)
+    dX, dgamma = add_rmsnorm_backward_rows(S, oracle.matmul(dY, W, trans_b=True), rstd, gamma, dS)
+    return S, oracle.matmul(N, W), dX, dgamma, oracle.matmul(N, dY, trans_a=True)

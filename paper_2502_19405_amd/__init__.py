@@ -7,6 +7,8 @@ The binding is imported on first use of one of its names so that the input
 generators can be imported without torch.
 """
 _BINDING_NAMES = ("matmul", "bmm", "bmm_raw", "softmax_rows", "layernorm_rows", "gelu", "exp",
+                  "add_rmsnorm_rows", "add_rmsnorm_quantize_rows", "add_rmsnorm_backward_rows",
+                  "quantize_rows", "matmul_q8", "sample_rows",
                   "Order", "Launch", "RepopsError", "gemm_configs", "abi_version", "load")
 
 

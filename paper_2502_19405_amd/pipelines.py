@@ -8,7 +8,10 @@ first product's epilogue (repops_matmul_gelu), and in the training step the
 GELU's input gradient by the epilogue of the product that makes its output
 gradient (repops_matmul_gelu_backward); both give the bits of the
 product and of the elementwise operator taken separately.  Every other
-intermediate comes from its own operator call.
+intermediate comes from its own operator call.  For a Llama program that generates
+tokens there are the feed-forward block with 8-bit products and the step from the
+last block's output to the next token, and for one that trains, the residual
+addition, norm and linear layer with their backward.
 """
 from __future__ import annotations
 
@@ -175,3 +178,52 @@ def mlp_train_step(state: MlpTrainState, X, dY, lr=1e-4, betas=(0.9, 0.999), eps
     repops.adam_step(state.param, state.grad, state.exp_avg, state.exp_avg_sq, lr, betas[0],
                      betas[1], eps, weight_decay, state.step, decoupled=True, order=order)
     return Y, dX
+
+
+def llama_feed_forward_q8(X, R, gamma, gate, up, down, eps=1e-5, order=None, keep=False):
+    """(S, D) of a Llama feed-forward block with 8-bit products: S = X + R, the
+    residual stream with the attention block's output, and
+    D = (silu(N Wg^T) * (N Wu^T)) Wd^T with N = rmsnorm(S).  gate, up [f, h] and
+    down [h, f] are (codes, scales) as repops.quantize_rows gives them of a weight
+    with one row per output feature; N and the products' inputs are quantised per
+    token.  S + D is the next block's residual stream: D is its R."""
+    S, Q, scale = repops.add_rmsnorm_quantize_rows(X, R, gamma, eps=eps, order=order)
+    G = repops.matmul_q8(Q, scale, *gate)
+    U = repops.matmul_q8(Q, scale, *up)
+    H = repops.swiglu(G, U, order=order)
+    HQ, h_scale = repops.quantize_rows(H)
+    D = repops.matmul_q8(HQ, h_scale, *down)
+    if keep:
+        return {"S": S, "Q": Q, "scale": scale, "G": G, "U": U, "H": H, "HQ": HQ,
+                "h_scale": h_scale, "D": D}
+    return S, D
+
+
+def llama_next_token(X, R, gamma, head, u, temperature=None, top_k=None, top_p=None, min_p=None,
+                     eps=1e-5, order=None, keep=False):
+    """(tokens, probabilities) that follow rows whose residual stream is X + R:
+    logits = rmsnorm(X + R) head^T by an 8-bit product (head [vocab, h] as codes
+    and scales), one token a row drawn with the numbers u (sample_rows)."""
+    _, Q, scale = repops.add_rmsnorm_quantize_rows(X, R, gamma, eps=eps, order=order)
+    logits = repops.matmul_q8(Q, scale, *head)
+    token, prob = repops.sample_rows(logits, u, temperature, top_k, top_p, min_p)
+    if keep:
+        return {"Q": Q, "scale": scale, "logits": logits, "token": token, "prob": prob}
+    return token, prob
+
+
+def norm_linear_forward(X, R, gamma, W, eps=1e-5, order=None, gemm_launch=None):
+    """(S, Y, saved): S = X + R and Y = rmsnorm(S) W, with what the backward needs."""
+    rstd = X.new_empty(X.shape[0])
+    S, N = repops.add_rmsnorm_rows(X, R, gamma, eps=eps, order=order, rstd_out=rstd)
+    Y = repops.matmul(N, W, order=order, launch=gemm_launch)
+    return S, Y, (S, N, rstd)
+
+
+def norm_linear_backward(saved, gamma, W, dY, dS=None, order=None, gemm_launch=None):
+    """(dX, dgamma, dW) of norm_linear_forward; dX is the gradient of X and of R.  dS
+    is the gradient that reaches S by its other uses, the residual stream's."""
+    S, N, rstd = saved
+    dN, dW = linear_backward(N, dY, W, order=order, gemm_launch=gemm_launch)
+    dX, dgamma = repops.add_rmsnorm_backward_rows(S, dN, rstd, gamma, dS, order=order)
+    return dX, dgamma, dW
