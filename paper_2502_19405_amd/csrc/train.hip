@@ -162,37 +162,52 @@ __device__ __forceinline__ void ln_bwd_terms(const RowBwdArgs& a, const float* x
   }
 }
 
-// The ADD forms' values of dS in the columns j0 + 64 t of one row: read ahead of the
-// row's reductions (+0 past the row) but behind the use of gamma, whose registers
-// they take (at the top of the row, 4096 columns need 132 registers: one workgroup per
-// compute unit instead of two), or, for 64 values a lane, at their use.  Nothing
-// otherwise.
-template <int T, bool ADD>
+// The gradient added to dX (RowBwdArgs::dS): none, one read as X and dY are, or one
+// read past the caches, which hold X and dY for their second reading; dS is read once.
+// Past the caches above 64 MB of matrices (4096 x 4096: 67 us against 75, dX alone 40
+// against 47; 4096 x 2048, 134 MB: 34.3 against 38.2), where smaller ones are slower
+// (4096 x 768, 50 MB: 16.4 against 15.2).
+enum { kNoAdd, kAdd, kAddOnce };
+
+template <class F>
+F pick_add(const RowBwdArgs& a, F none, F add, F once) {
+  if (!a.dS) return none;
+  return a.rows * a.cols > (int64_t(64) << 20) / 16 ? once : add;
+}
+
+// The values of dS in the columns j0 + 64 t of one row: read ahead of the row's
+// reductions (+0 past the row) but behind the use of gamma, whose registers they take,
+// or, for 64 values a lane, at their use.
+template <int T, int ADD>
 struct AddRow {
   static constexpr bool kPre = ADD && T <= 32;
   float v[kPre ? T : 1];
   const float* ds;
+  __device__ __forceinline__ float at(int t) const {
+    if constexpr (ADD == kAddOnce) return __builtin_nontemporal_load(ds + kWave * t);
+    else return ds[kWave * t];
+  }
   __device__ __forceinline__ void load(const RowBwdArgs& a, int64_t row, int64_t j0) {
     if constexpr (ADD) ds = a.dS + row * a.ldds + j0;
     if constexpr (kPre) {
 #pragma unroll
       for (int t = 0; t < T; ++t) {
         v[t] = 0.0f;
-        if (j0 + kWave * t < a.cols) v[t] = ds[kWave * t];
+        if (j0 + kWave * t < a.cols) v[t] = at(t);
       }
     }
   }
   // (column j0 + 64 t is within the row)
   __device__ __forceinline__ float operator()(int t, float dx) const {
     if constexpr (kPre) return dx + v[t];
-    else if constexpr (ADD) return dx + ds[kWave * t];
+    else if constexpr (ADD) return dx + at(t);
     else return dx;
   }
 };
 
 // dX of one row by one wave (row < a.rows, uniform over the wave; all 64
 // lanes active).
-template <int T, bool ADD>
+template <int T, int ADD>
 __device__ __forceinline__ void layernorm_bwd_row(const RowBwdArgs& a, int64_t row, int lane) {
   const float* x = a.Y + row * a.ldy;
   const float* dy = a.dY + row * a.lddy;
@@ -230,7 +245,7 @@ __device__ __forceinline__ void layernorm_bwd_row(const RowBwdArgs& a, int64_t r
   }
 }
 
-template <int T, bool ADD>
+template <int T, int ADD>
 __global__ __launch_bounds__(512) void layernorm_bwd_wave_kernel(RowBwdArgs a, int wpb) {
   const int lane = threadIdx.x & (kWave - 1);
   const int64_t row = static_cast<int64_t>(blockIdx.x) * wpb + wave_id();
@@ -289,7 +304,7 @@ __global__ __launch_bounds__(512) void softmax_bwd_split_kernel(RowBwdArgs a) {
   }
 }
 
-template <int T, bool ADD>
+template <int T, int ADD>
 __global__ __launch_bounds__(512) void layernorm_bwd_split_kernel(RowBwdArgs a) {
   __shared__ float chain_g[kWave];
   __shared__ float chain_gt[kWave];
@@ -546,7 +561,7 @@ __global__ __launch_bounds__(NT) void layernorm_param_combine_kernel(LnParamArgs
 
 constexpr int kFusedChains = 4;  // columns per thread in the chain phase
 
-template <int T, int MAXT, bool PF, bool ADD>
+template <int T, int MAXT, bool PF, int ADD>
 __global__ __launch_bounds__(MAXT) void layernorm_bwd_fused_kernel(RowBwdArgs a, LnParamArgs p,
                                                                    int R, int64_t nblk) {
   extern __shared__ float stage[];  // [R][cols] t, then [R][cols] dy
@@ -693,7 +708,7 @@ constexpr int kSplitWaves = 8;
 // the results are the same bits.  Every wave takes part in every step (the
 // steps hold workgroup barriers); a group past end works on row first and
 // stores nothing.
-template <int T, int S, bool ADD>
+template <int T, int S, int ADD>
 __device__ __forceinline__ void layernorm_bwd_rows_grouped(const RowBwdArgs& a, int64_t first,
                                                            int64_t stride, int64_t end, int lane,
                                                            int w) {
@@ -761,7 +776,7 @@ __device__ __forceinline__ void layernorm_bwd_rows_grouped(const RowBwdArgs& a, 
 // one wave measured faster than two of 16).
 constexpr int kColsplitGroupT = 16;
 
-template <int T, int SWU, bool ADD>
+template <int T, int SWU, int ADD>
 __global__ __launch_bounds__(kSplitWaves * kWave) void layernorm_bwd_colsplit_kernel(
     RowBwdArgs a, LnParamArgs p, int G, int slice, int64_t nblk) {
   constexpr int SW = kWave * SWU;            // LDS pitch: slice columns at most
@@ -968,7 +983,7 @@ WaveBwdKernel pick_softmax_bwd(int64_t cols) {
   return softmax_bwd_wave_kernel<64>;
 }
 
-template <bool ADD>
+template <int ADD>
 WaveBwdKernel pick_layernorm_bwd(int64_t cols) {
   if (cols <= kWave * 1) return layernorm_bwd_wave_kernel<1, ADD>;
   if (cols <= kWave * 2) return layernorm_bwd_wave_kernel<2, ADD>;
@@ -994,8 +1009,9 @@ SplitBwdKernel pick_split_bwd(int64_t cols, int S) {
   return nullptr;
 }
 template <int T> struct SoftmaxBwdSplit { static constexpr SplitBwdKernel fn = softmax_bwd_split_kernel<T>; };
-template <int T> struct LayernormBwdSplit { static constexpr SplitBwdKernel fn = layernorm_bwd_split_kernel<T, false>; };
-template <int T> struct LayernormAddBwdSplit { static constexpr SplitBwdKernel fn = layernorm_bwd_split_kernel<T, true>; };
+template <int T> struct LayernormBwdSplit { static constexpr SplitBwdKernel fn = layernorm_bwd_split_kernel<T, kNoAdd>; };
+template <int T> struct LayernormAddBwdSplit { static constexpr SplitBwdKernel fn = layernorm_bwd_split_kernel<T, kAdd>; };
+template <int T> struct LayernormAddOnceBwdSplit { static constexpr SplitBwdKernel fn = layernorm_bwd_split_kernel<T, kAddOnce>; };
 
 hipError_t launch_split_bwd(SplitBwdKernel k, const RowBwdArgs& a, int S, hipStream_t s) {
   if (!k) return hipErrorInvalidValue;
@@ -1009,7 +1025,7 @@ using FusedKernel = void (*)(RowBwdArgs, LnParamArgs, int, int64_t);
 
 // Kernels for R <= 8 waves (512 threads); the widest rows (32 values per
 // lane) load each row at the top of its pass instead of one pass ahead.
-template <bool ADD>
+template <int ADD>
 FusedKernel pick_layernorm_fused(int64_t cols) {
   if (cols <= kWave * 1) return layernorm_bwd_fused_kernel<1, 512, true, ADD>;
   if (cols <= kWave * 2) return layernorm_bwd_fused_kernel<2, 512, true, ADD>;
@@ -1053,7 +1069,8 @@ hipError_t launch_softmax_bwd_generic(const RowBwdArgs& a, hipStream_t s) {
 
 hipError_t launch_layernorm_bwd_wave(const RowBwdArgs& a, int wpb, hipStream_t s) {
   const int64_t blocks = (a.rows + wpb - 1) / wpb;
-  const WaveBwdKernel k = a.dS ? pick_layernorm_bwd<true>(a.cols) : pick_layernorm_bwd<false>(a.cols);
+  const WaveBwdKernel k = pick_add(a, pick_layernorm_bwd<kNoAdd>, pick_layernorm_bwd<kAdd>,
+                                    pick_layernorm_bwd<kAddOnce>)(a.cols);
   hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(blocks)),
                      dim3(kWave * wpb), 0, s, a, wpb);
   return hipGetLastError();
@@ -1064,8 +1081,9 @@ hipError_t launch_softmax_bwd_split(const RowBwdArgs& a, int S, hipStream_t s) {
 }
 
 hipError_t launch_layernorm_bwd_split(const RowBwdArgs& a, int S, hipStream_t s) {
-  const SplitBwdKernel k = a.dS ? pick_split_bwd<LayernormAddBwdSplit>(a.cols, S)
-                                : pick_split_bwd<LayernormBwdSplit>(a.cols, S);
+  const SplitBwdKernel k =
+      pick_add(a, pick_split_bwd<LayernormBwdSplit>, pick_split_bwd<LayernormAddBwdSplit>,
+               pick_split_bwd<LayernormAddOnceBwdSplit>)(a.cols, S);
   return launch_split_bwd(k, a, S, s);
 }
 
@@ -1143,7 +1161,8 @@ hipError_t launch_layernorm_bwd_fused(const RowBwdArgs& a, const LnParamArgs& p,
   const int64_t nblk = layernorm_param_blocks(a.rows, p.k_block);
   const size_t lds = sizeof(float) * 2 * static_cast<size_t>(R) * static_cast<size_t>(a.cols);
   const FusedKernel k =
-      a.dS ? pick_layernorm_fused<true>(a.cols) : pick_layernorm_fused<false>(a.cols);
+      pick_add(a, pick_layernorm_fused<kNoAdd>, pick_layernorm_fused<kAdd>,
+               pick_layernorm_fused<kAddOnce>)(a.cols);
   hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(nblk)),
                      dim3(R * kWave), lds, s, a, p, R, nblk);
   hipError_t e = hipGetLastError();
@@ -1153,7 +1172,7 @@ hipError_t launch_layernorm_bwd_fused(const RowBwdArgs& a, const LnParamArgs& p,
 
 using ColsplitKernel = void (*)(RowBwdArgs, LnParamArgs, int, int, int64_t);
 
-template <int SWU, bool ADD>
+template <int SWU, int ADD>
 ColsplitKernel pick_colsplit_t(int64_t cols) {
   if (cols <= kWave * 1) return layernorm_bwd_colsplit_kernel<1, SWU, ADD>;
   if (cols <= kWave * 2) return layernorm_bwd_colsplit_kernel<2, SWU, ADD>;
@@ -1165,7 +1184,7 @@ ColsplitKernel pick_colsplit_t(int64_t cols) {
   return layernorm_bwd_colsplit_kernel<64, SWU, ADD>;
 }
 
-template <bool ADD>
+template <int ADD>
 ColsplitKernel pick_colsplit(int64_t cols, int swu) {
   return swu == 1   ? pick_colsplit_t<1, ADD>(cols)
          : swu == 2 ? pick_colsplit_t<2, ADD>(cols)
@@ -1196,7 +1215,8 @@ hipError_t launch_layernorm_bwd_colsplit(const RowBwdArgs& a, const LnParamArgs&
                                          const ColsplitPlan& pl, hipStream_t s) {
   const int64_t nblk = layernorm_param_blocks(a.rows, p.k_block);
   const ColsplitKernel k =
-      a.dS ? pick_colsplit<true>(a.cols, pl.swu) : pick_colsplit<false>(a.cols, pl.swu);
+      pick_add(a, pick_colsplit<kNoAdd>, pick_colsplit<kAdd>, pick_colsplit<kAddOnce>)(a.cols,
+                                                                                       pl.swu);
   hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(nblk * pl.G)), dim3(kSplitWaves * kWave), 0,
                      s, a, p, pl.G, pl.slice, nblk);
   hipError_t e = hipGetLastError();
