@@ -899,7 +899,12 @@ def _matrix(t, shape, dtype, device: int, name: str):
         return None, 0
     if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)} (got {list(t.shape)})")
-    return _at(t, dtype, device, name), _row_major(t, name)[2]
+    ld, step = t.stride()
+    if step != 1 or ld < shape[1]:  # (one row or column, or a refusal)
+        ld = _row_major(t, name)[2]
+    if t.dtype is dtype and t.get_device() == device >= 0:
+        return t.data_ptr(), ld
+    return _at(t, dtype, device, name), ld
 
 
 def _vector(t, size: int, dtype, device: int, name: str):
