@@ -354,9 +354,11 @@ __device__ __forceinline__ uint64_t entry_of(uint32_t key, int j) {
 }
 
 // A bucket with more tokens than kSmall: its keys' interval is cut into kSub parts
-// again and again, until the part that holds `at` is small or a single key.
-__device__ __noinline__ Found among_many(Shared& sh, const Row<kThreads>& row, const Scale& sc, int bucket, bool by_count,
-                            uint64_t at, uint64_t before, uint64_t place) {
+// again and again, until the part that holds `at` is small or a single key.  True: that
+// part's tokens are in sh.small, behind `before` and `place`; otherwise f is the token.
+__device__ __forceinline__ bool narrow(Shared& sh, const Row<kThreads>& row, const Scale& sc,
+                                       int bucket, bool by_count, uint64_t at, uint64_t& before,
+                                       uint64_t& place, Found& f) {
   const int tid = threadIdx.x;
   if (tid == 0) {
     sh.lo = 0xffffffffu;
@@ -439,7 +441,7 @@ __device__ __noinline__ Found among_many(Shared& sh, const Row<kThreads>& row, c
       if (k >= lo && k <= hi) sh.small[atomicAdd(&sh.n_small, 1u)].x = entry_of(k, j);
     });
     __syncthreads();
-    return among_small(sh, sc, by_count, at, before, place);
+    return true;
   }
   // Equal logits, as many as there are: the place among them in order of the index.
   // The indices are cut into kSub parts in the same way.
@@ -476,19 +478,23 @@ __device__ __noinline__ Found among_many(Shared& sh, const Row<kThreads>& row, c
     span = part;
     __syncthreads();
   }
-  return {before + want * w, w, first};
+  f = {before + want * w, w, first};
+  return false;
 }
 
-// The tokens that `in` takes, at most four a thread at a time, into the list (as far
-// as they fit); sh.n_list counts them.
+// The tokens that `in` takes into the list, as far as they fit; sh.n_list counts them.
 template <class In>
 __device__ __forceinline__ void collect(Shared& sh, const Row<kThreads>& row, In in) {
+  // An address the compiler takes for a lane's own: LDS adds the lanes' counts one
+  // after the other faster than the scan that it would put in their place.
+  uint32_t own = 0;
+  asm volatile("" : "+v"(own));
   row.each4<4>([&](const float (&x)[4], int j, int count) {
     uint32_t taken = 0;
 #pragma unroll
     for (int k = 0; k < 4; ++k) taken += k < count && in(x[k]);
     if (taken) {
-      uint32_t i = atomicAdd(&sh.n_list, taken);
+      uint32_t i = atomicAdd(&sh.n_list + own, taken);
 #pragma unroll
       for (int k = 0; k < 4; ++k)
         if (k < count && in(x[k])) {
@@ -509,8 +515,9 @@ __device__ Found locate(Shared& sh, const Row<kThreads>& row, const Scale& sc, b
                         Listed& listed) {
   const int tid = threadIdx.x;
   const int bucket = part_of(sh, sh.before, sh.places, kBuckets, by_count, at);
-  const uint64_t before = sh.before[bucket];
-  const uint64_t place = counted ? sh.places[bucket] : 0;
+  uint64_t before = sh.before[bucket];
+  uint64_t place = counted ? sh.places[bucket] : 0;
+  bool many = false;
   if (!listed.holds(bucket)) {
     listed = {bucket, bucket, 0, -1, 0};
     const int beyond = bucket + 3 < kBuckets ? bucket + 3 : kBuckets;  // past the neighbours'
@@ -540,26 +547,26 @@ __device__ Found locate(Shared& sh, const Row<kThreads>& row, const Scale& sc, b
     }
     __syncthreads();
     listed.n = sh.n_list;
-    if (listed.n > kList) {
-      listed = {0, -1, 0, -1, 0};
-      return among_many(sh, row, sc, bucket, by_count, at, before, place);
-    }
+    many = listed.n > kList;
   }
-  // the bucket's own among the collected
-  if (tid == 0) sh.n_small = 0;
-  __syncthreads();
-  for (uint32_t i = tid; i < listed.n; i += kThreads) {
-    const uint64_t e = sh.list[i];
-    if (sc.bucket(logit_of(static_cast<uint32_t>(e >> 32))) == bucket) {
-      const uint32_t k = atomicAdd(&sh.n_small, 1u);
-      if (k < kSmall) sh.small[k].x = e;
+  if (!many) {  // the bucket's own among the collected
+    if (tid == 0) sh.n_small = 0;
+    __syncthreads();
+    for (uint32_t i = tid; i < listed.n; i += kThreads) {
+      const uint64_t e = sh.list[i];
+      if (sc.bucket(logit_of(static_cast<uint32_t>(e >> 32))) == bucket) {
+        const uint32_t k = atomicAdd(&sh.n_small, 1u);
+        if (k < kSmall) sh.small[k].x = e;
+      }
     }
+    __syncthreads();
+    many = sh.n_small > kSmall;
   }
-  __syncthreads();
-  if (sh.n_small > kSmall) {
+  if (many) {
     __syncthreads();
     listed = {0, -1, 0, -1, 0};
-    return among_many(sh, row, sc, bucket, by_count, at, before, place);
+    Found f;
+    if (!narrow(sh, row, sc, bucket, by_count, at, before, place, f)) return f;
   }
   return among_small(sh, sc, by_count, at, before, place);
 }
@@ -721,17 +728,14 @@ __device__ __forceinline__ Scale scale_of(const Params& p, float m) {
 // One workgroup a row.
 __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
   __shared__ Shared sh;
-  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-    const Row<kThreads> row = {a.L + r * a.ldl, static_cast<int>(a.vocab)};
-    const Params p(a, r);
-    const float m = find_top(row, sh.wave_m);
-    if (!pick_plain(a, sh.wave_c, r, p, m)) {
-      const Scale sc = scale_of(p, m);
-      const uint64_t near = weigh(sh, sh.table, row, p, sc, p.counted(a.vocab));
-      pick(a, sh, r, p, sc, near);
-    }
-    __syncthreads();  // what the next row overwrites has been read
-  }
+  const int64_t r = blockIdx.x;
+  const Row<kThreads> row = {a.L + r * a.ldl, static_cast<int>(a.vocab)};
+  const Params p(a, r);
+  const float m = find_top(row, sh.wave_m);
+  if (pick_plain(a, sh.wave_c, r, p, m)) return;
+  const Scale sc = scale_of(p, m);
+  const uint64_t near = weigh(sh, sh.table, row, p, sc, p.counted(a.vocab));
+  pick(a, sh, r, p, sc, near);
 }
 
 // Long rows: a stretch of `stretch` tokens of a row per workgroup in the first two
@@ -786,6 +790,20 @@ __global__ __launch_bounds__(kWeighThreads) void sample_weigh_kernel(SampleArgs 
   if (threadIdx.x == 0) part.near = near;
 }
 
+// A sum over a row's parts, eight loads ahead of their use.
+template <class Of>
+__device__ __forceinline__ auto sum_parts(const Part* part, int G, Of of) {
+  decltype(of(*part)) sum = 0, v[8];
+#pragma nounroll
+  for (int g = 0; g < G; g += 8) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = of(part[g + k < G ? g + k : G - 1]);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum += g + k < G ? v[k] : 0;
+  }
+  return sum;
+}
+
 __global__ __launch_bounds__(kThreads) void sample_pick_kernel(SampleArgs a, const Part* parts,
                                                                int G) {
   __shared__ Shared sh;
@@ -796,20 +814,10 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(SampleArgs a, con
   if (pick_plain(a, sh.wave_c, r, p, m)) return;
   const bool counted = p.counted(a.vocab);
   for (int b = threadIdx.x; b < kBuckets; b += kThreads) {
-    uint64_t w = 0;
-    uint32_t c = 0;
-    if (counted) {
-#pragma unroll 8
-      for (int g = 0; g < G; ++g) c += part[g].count[b];
-    }
-#pragma unroll 8
-    for (int g = 0; g < G; ++g) w += part[g].weight[b];
-    sh.before[b] = w;
-    sh.places[b] = c;
+    sh.before[b] = sum_parts(part, G, [&](const Part& q) { return q.weight[b]; });
+    sh.places[b] = counted ? sum_parts(part, G, [&](const Part& q) { return q.count[b]; }) : 0;
   }
-  uint64_t near = 0;
-  if (p.use_m())
-    for (int g = 0; g < G; ++g) near += part[g].near;
+  const uint64_t near = p.use_m() ? sum_parts(part, G, [](const Part& q) { return q.near; }) : 0;
   __syncthreads();
   pick(a, sh, r, p, scale_of(p, m), near);
 }
@@ -848,13 +856,9 @@ uint64_t sample_workspace_bytes(int64_t rows, int64_t vocab) {
 }
 
 hipError_t launch_sample(const SampleArgs& a, void* workspace, hipStream_t s) {
-  if (a.vocab <= kOneLaunch) {
-    const int64_t cap = int64_t(1) << 20;
-    hipLaunchKernelGGL(sample_kernel, dim3(static_cast<unsigned>(a.rows < cap ? a.rows : cap)),
-                       dim3(kThreads), 0, s, a);
-    return hipGetLastError();
-  }
-  const Plan p = plan_of(a.rows, a.vocab);
+  const bool one = a.vocab <= kOneLaunch;
+  Plan p{int64_t(1) << 20, 1, 0};  // (a launch has fewer than 2^32 threads)
+  if (!one) p = plan_of(a.rows, a.vocab);
   Part* parts = static_cast<Part*>(workspace);
   for (int64_t r0 = 0; r0 < a.rows; r0 += p.group) {
     SampleArgs g = a;
@@ -868,10 +872,15 @@ hipError_t launch_sample(const SampleArgs& a, void* workspace, hipStream_t s) {
     g.token = a.token + r0;
     if (a.prob) g.prob = a.prob + r0;
     const dim3 wide(static_cast<unsigned>(g.rows * p.G)), rows(static_cast<unsigned>(g.rows));
-    hipLaunchKernelGGL(sample_top_kernel, wide, dim3(kWeighThreads), 0, s, g, parts, p.G, p.stretch);
-    hipLaunchKernelGGL(sample_weigh_kernel, wide, dim3(kWeighThreads), 0, s, g, parts, p.G,
-                       p.stretch);
-    hipLaunchKernelGGL(sample_pick_kernel, rows, dim3(kThreads), 0, s, g, parts, p.G);
+    if (one) {
+      hipLaunchKernelGGL(sample_kernel, rows, dim3(kThreads), 0, s, g);
+    } else {
+      hipLaunchKernelGGL(sample_top_kernel, wide, dim3(kWeighThreads), 0, s, g, parts, p.G,
+                         p.stretch);
+      hipLaunchKernelGGL(sample_weigh_kernel, wide, dim3(kWeighThreads), 0, s, g, parts, p.G,
+                         p.stretch);
+      hipLaunchKernelGGL(sample_pick_kernel, rows, dim3(kThreads), 0, s, g, parts, p.G);
+    }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
