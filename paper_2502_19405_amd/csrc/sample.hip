@@ -15,10 +15,10 @@
 //
 // A row is walked for its maximum, for the buckets' weights and for the tokens of the
 // buckets wanted (a float comparison rejects most others).  The second walk is bound by
-// instruction issue (about 35 a token), the others by memory.  Rows of up to 16384
-// tokens take one workgroup and one launch; longer ones a launch for each walk, the
-// first two with several workgroups a row where rows are few, in groups of rows whose
-// logits stay in the 256 MB cache from one walk to the next.
+// instruction issue (about 35 a token), the others by memory.  One workgroup does a row
+// in one launch; of few long rows a launch does each walk, the first two with several
+// workgroups a row, in groups of rows whose logits stay in the 256 MB cache from one
+// walk to the next.  512 x 131072: 149 us, 42 for one reading; 1 x 128000: 30 us.
 #include <hip/hip_runtime.h>
 
 #include "generation_internal.h"
@@ -199,11 +199,20 @@ struct Row {
       f(x, j, n - j < 4 ? n - j : 4);
     }
   }
-  // f(logit, index) for every token, one at a time.
-  template <class F>
+  // f(logit, index) for every token, one at a time, U loads ahead of their use.
+  template <int U, class F>
   __device__ __forceinline__ void each(F f) const {
+    int j = static_cast<int>(threadIdx.x);
 #pragma nounroll
-    for (int j = static_cast<int>(threadIdx.x); j < n; j += NT) f(l[j], j);
+    for (; j + (U - 1) * NT < n; j += U * NT) {
+      float x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) x[u] = l[j + u * NT];
+#pragma unroll
+      for (int u = 0; u < U; ++u) f(x[u], j + u * NT);
+    }
+#pragma nounroll
+    for (; j < n; j += NT) f(l[j], j);
   }
 };
 
@@ -366,8 +375,9 @@ __device__ __forceinline__ bool narrow(Shared& sh, const Row<kThreads>& row, con
   }
   __syncthreads();
   uint32_t least = 0xffffffffu, most = 0;
-  row.each([&](float l, int) {
-    if (sc.bucket(l) == bucket) {
+  const Interval near = {sc, bucket, bucket};
+  row.each<8>([&](float l, int) {
+    if (near(l) && sc.bucket(l) == bucket) {
       const uint32_t k = key_of(l);
       least = k < least ? k : least;
       most = k > most ? k : most;
@@ -386,7 +396,7 @@ __device__ __forceinline__ bool narrow(Shared& sh, const Row<kThreads>& row, con
     sh.sub_w[tid] = 0;
     sh.sub_c[tid] = 0;
     __syncthreads();
-    row.each([&](float l, int) {
+    row.each<8>([&](float l, int) {
       const uint32_t k = key_of(l);
       if (k >= lo && k <= hi) {
         const uint32_t b = (hi - k) >> shift;
@@ -436,7 +446,7 @@ __device__ __forceinline__ bool narrow(Shared& sh, const Row<kThreads>& row, con
     __syncthreads();
     if (tid == 0) sh.n_small = 0;
     __syncthreads();
-    row.each([&](float l, int j) {
+    row.each<8>([&](float l, int j) {
       const uint32_t k = key_of(l);
       if (k >= lo && k <= hi) sh.small[atomicAdd(&sh.n_small, 1u)].x = entry_of(k, j);
     });
@@ -454,7 +464,7 @@ __device__ __forceinline__ bool narrow(Shared& sh, const Row<kThreads>& row, con
     __syncthreads();
     sh.sub_c[tid] = 0;
     __syncthreads();
-    row.each([&](float l, int j) {
+    row.each<8>([&](float l, int j) {
       const uint32_t at_j = static_cast<uint32_t>(j) - first;
       if (at_j < span && key_of(l) == lo) atomicAdd(&sh.sub_c[at_j / part], 1u);
     });
@@ -845,18 +855,26 @@ Plan plan_of(int64_t rows, int64_t vocab) {
   return p;
 }
 
-constexpr int64_t kOneLaunch = 16384;  // longest row of the single launch
+// One launch, a workgroup a row, takes about 0.36 us per 1000 tokens and round over the
+// compute units; sharing a row's first two walks out saves 0.25 of that as far as units
+// are free, and costs 12 us of launches and partial sums: 48000 tokens of one row
+// (1 x 50000: 22.5 us in one launch, 21.6 in three; 1 x 128000: 52 and 30; 128 x 64000:
+// 33 and 40; 128 x 128000: 69 and 63; 256 x 128000: 84 and 93).
+bool one_launch(int64_t rows, int64_t vocab) {
+  constexpr int64_t kUnits = 256;
+  return rows >= kUnits || vocab * (kUnits - rows) <= 48000 * kUnits;
+}
 
 }  // namespace
 
 uint64_t sample_workspace_bytes(int64_t rows, int64_t vocab) {
-  if (vocab <= kOneLaunch || rows <= 0) return 0;
+  if (rows <= 0 || one_launch(rows, vocab)) return 0;
   const Plan p = plan_of(rows, vocab);
   return static_cast<uint64_t>(p.group) * static_cast<uint64_t>(p.G) * sizeof(Part);
 }
 
 hipError_t launch_sample(const SampleArgs& a, void* workspace, hipStream_t s) {
-  const bool one = a.vocab <= kOneLaunch;
+  const bool one = one_launch(a.rows, a.vocab);
   Plan p{int64_t(1) << 20, 1, 0};  // (a launch has fewer than 2^32 threads)
   if (!one) p = plan_of(a.rows, a.vocab);
   Part* parts = static_cast<Part*>(workspace);

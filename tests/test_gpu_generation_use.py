@@ -105,7 +105,7 @@ def test_graphs_replay_a_generation_step(rp):
     import torch
 
     from paper_2502_19405_amd import pipelines
-    sizes = ((3, 256, 512, 40000), (40, 128, 384, 17000))
+    sizes = ((3, 256, 512, 60000), (40, 128, 384, 70000))
     ds = [on_device(program(3200 + i, *s)) for i, s in enumerate(sizes)]
     announce("graph", "capture")
     graphs = [capture(lambda d=d: generate(pipelines, d)) for d in ds]
@@ -175,7 +175,7 @@ def test_other_streams_and_calls_at_once(rp):
     import torch
     g = inputs.rng(3400)
     jobs = []
-    for rows, vocab in ((40, 60000), (3, 128000)):
+    for rows, vocab in ((20, 90000), (3, 128000)):
         L, u = inputs.normal(g, (rows, vocab), var=6.0), g.random(rows, dtype=np.float32)
         p = np.full(rows, 0.9, np.float32)
         jobs.append((L, u, p, generation.sample_rows(L, u, top_p=p)))
