@@ -18,7 +18,7 @@
 // instruction issue (about 35 a token), the others by memory.  One workgroup does a row
 // in one launch; of few long rows a launch does each walk, the first two with several
 // workgroups a row, in groups of rows whose logits stay in the 256 MB cache from one
-// walk to the next.  512 x 131072: 149 us, 42 for one reading; 1 x 128000: 30 us.
+// walk to the next.  512 x 131072: 140 us, 42 for one reading; 1 x 128000: 30 us.
 #include <hip/hip_runtime.h>
 
 #include "generation_internal.h"
@@ -29,15 +29,15 @@
 namespace repops {
 namespace {
 
-constexpr int kThreads = 1024;       // of the workgroup that picks a row's token
+constexpr int kThreads = 1024;       // of a workgroup that picks a row's token, or 512
 constexpr int kWeighThreads = 512;   // of those that share a long row's first walks
 constexpr double kSpan = 31.0;        // exp(-31) < 2^-44: a weight of 0
 constexpr int kPerUnit = 64;          // buckets per unit of d
 constexpr int kWeighted = 31 * kPerUnit + 1;  // buckets 0 .. 1984: rint(64 * 31)
 constexpr int kBuckets = kWeighted + 1;       // the last one: weight 0
 constexpr int kList = 4096;           // tokens collected at once
-constexpr int kSmall = kThreads;      // tokens put in order at once
-constexpr int kSub = 1024;            // parts that a bucket's keys are narrowed by
+constexpr int kSmall = kThreads;      // tokens put in order at once, one a thread
+constexpr int kSub = kThreads;        // parts that a bucket's keys are narrowed by, likewise
 
 // exp(d) 2^43 for d in [-31, 0]: the degree-11 Taylor polynomial is within 7e-15
 // of exp.
@@ -229,12 +229,12 @@ __device__ T block_reduce(T v, T* per_wave, Op op) {
 }
 
 // What stands in the waves before this one.
-template <class T>
+template <int NT, class T>
 __device__ __forceinline__ T waves_before(const T* per_wave) {
   const int wave = threadIdx.x >> 6;
   T sum = 0;
 #pragma unroll
-  for (int k = 0; k < kThreads / 64 - 1; ++k) sum += k < wave ? per_wave[k] : T(0);
+  for (int k = 0; k < NT / 64 - 1; ++k) sum += k < wave ? per_wave[k] : T(0);
   return sum;
 }
 
@@ -242,14 +242,24 @@ __device__ __forceinline__ void add_u64(uint64_t* p, uint64_t v) {
   atomicAdd(reinterpret_cast<unsigned long long*>(p), static_cast<unsigned long long>(v));
 }
 
-// before[] and places[] of `buckets` parts (at most 2 a thread) become the running
-// sums before each part, the total in entry `buckets`.
-__device__ void running(Shared& sh, uint64_t* w, uint32_t* c, int buckets) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = tid * 2;
-  const uint64_t w0 = b < buckets ? w[b] : 0, w1 = b + 1 < buckets ? w[b + 1] : 0;
-  const uint32_t c0 = b < buckets ? c[b] : 0, c1 = b + 1 < buckets ? c[b + 1] : 0;
-  uint64_t sw = w0 + w1;
-  uint32_t sc = c0 + c1;
+// The buckets' weights and counts become the running sums before each, the totals
+// in the entry behind the last.
+template <int NT>
+__device__ void running(Shared& sh) {
+  constexpr int kOwn = (kBuckets + NT) / NT;  // a thread's neighbouring buckets
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  uint64_t w[kOwn], sw = 0;
+  uint32_t c[kOwn], sc = 0;
+#pragma unroll
+  for (int k = 0; k < kOwn; ++k) {
+    const int b = tid * kOwn + k;
+    w[k] = b < kBuckets ? sh.before[b] : 0;
+    c[k] = b < kBuckets ? sh.places[b] : 0;
+    sw += w[k];
+    sc += c[k];
+  }
+  uint64_t own_w = sw;
+  uint32_t own_c = sc;
   for (int s = 1; s < 64; s <<= 1) {
     const uint64_t ow = __shfl_up(sw, s);
     const uint32_t oc = __shfl_up(sc, s);
@@ -263,23 +273,27 @@ __device__ void running(Shared& sh, uint64_t* w, uint32_t* c, int buckets) {
     sh.wave_c[wave] = sc;
   }
   __syncthreads();
-  sw += waves_before(sh.wave_w);
-  sc += waves_before(sh.wave_c);
-  if (b <= buckets) {
-    w[b] = sw - w0 - w1;
-    c[b] = sc - c0 - c1;
-  }
-  if (b + 1 <= buckets) {
-    w[b + 1] = sw - w1;
-    c[b + 1] = sc - c1;
+  sw += waves_before<NT>(sh.wave_w) - own_w;
+  sc += waves_before<NT>(sh.wave_c) - own_c;
+#pragma unroll
+  for (int k = 0; k < kOwn; ++k) {
+    const int b = tid * kOwn + k;
+    if (b <= kBuckets) {
+      sh.before[b] = sw;
+      sh.places[b] = sc;
+    }
+    sw += w[k];
+    sc += c[k];
   }
   __syncthreads();
 }
 
-// The part whose running sums hold `at`.
-__device__ int part_of(Shared& sh, const uint64_t* w, const uint32_t* c, int buckets, bool by_count,
-                       uint64_t at) {
-  for (int b = threadIdx.x; b < buckets; b += kThreads)
+// The bucket whose running sums hold `at`.
+template <int NT>
+__device__ int part_of(Shared& sh, bool by_count, uint64_t at) {
+  const uint64_t* w = sh.before;
+  const uint32_t* c = sh.places;
+  for (int b = threadIdx.x; b < kBuckets; b += NT)
     if (by_count ? at >= c[b] && at < c[b + 1] : at >= w[b] && at < w[b + 1]) sh.found_bucket = b;
   __syncthreads();
   const int b = sh.found_bucket;
@@ -328,6 +342,7 @@ struct Listed {
 // The token at `at` (weight or place before it) among the sh.n_small tokens of
 // sh.small, which follow `before` weight and `place` tokens: every token's place
 // by comparison with the others.
+template <int NT>
 __device__ Found among_small(Shared& sh, const Scale& sc, bool by_count, uint64_t at,
                              uint64_t before, uint64_t place) {
   const uint32_t n = sh.n_small, i = threadIdx.x;
@@ -362,10 +377,11 @@ __device__ __forceinline__ uint64_t entry_of(uint32_t key, int j) {
   return static_cast<uint64_t>(key) << 32 | (0xffffffffu - static_cast<uint32_t>(j));
 }
 
-// A bucket with more tokens than kSmall: its keys' interval is cut into kSub parts
+// A bucket with more tokens than threads: its keys' interval is cut into as many parts
 // again and again, until the part that holds `at` is small or a single key.  True: that
 // part's tokens are in sh.small, behind `before` and `place`; otherwise f is the token.
-__device__ __forceinline__ bool narrow(Shared& sh, const Row<kThreads>& row, const Scale& sc,
+template <int NT>
+__device__ __forceinline__ bool narrow(Shared& sh, const Row<NT>& row, const Scale& sc,
                                        int bucket, bool by_count, uint64_t at, uint64_t& before,
                                        uint64_t& place, Found& f) {
   const int tid = threadIdx.x;
@@ -376,7 +392,7 @@ __device__ __forceinline__ bool narrow(Shared& sh, const Row<kThreads>& row, con
   __syncthreads();
   uint32_t least = 0xffffffffu, most = 0;
   const Interval near = {sc, bucket, bucket};
-  row.each<8>([&](float l, int) {
+  row.template each<8>([&](float l, int) {
     if (near(l) && sc.bucket(l) == bucket) {
       const uint32_t k = key_of(l);
       least = k < least ? k : least;
@@ -388,15 +404,15 @@ __device__ __forceinline__ bool narrow(Shared& sh, const Row<kThreads>& row, con
     atomicMax(&sh.hi, most);
   }
   __syncthreads();
-  uint32_t lo = sh.lo, hi = sh.hi, held = kSmall + 1;
-  while (held > kSmall && lo != hi) {
+  uint32_t lo = sh.lo, hi = sh.hi, held = NT + 1;
+  while (held > NT && lo != hi) {
     int shift = 0;
-    while (((hi - lo) >> shift) >= kSub) ++shift;
+    while (((hi - lo) >> shift) >= NT) ++shift;
     __syncthreads();
     sh.sub_w[tid] = 0;
     sh.sub_c[tid] = 0;
     __syncthreads();
-    row.each<8>([&](float l, int) {
+    row.template each<8>([&](float l, int) {
       const uint32_t k = key_of(l);
       if (k >= lo && k <= hi) {
         const uint32_t b = (hi - k) >> shift;
@@ -423,8 +439,8 @@ __device__ __forceinline__ bool narrow(Shared& sh, const Row<kThreads>& row, con
       sh.wave_c[tid >> 6] = bc;
     }
     __syncthreads();
-    bw += waves_before(sh.wave_w);
-    bc += waves_before(sh.wave_c);
+    bw += waves_before<NT>(sh.wave_w);
+    bc += waves_before<NT>(sh.wave_c);
     bw = bw - w + before;
     const uint64_t bp = bc - c + place;
     if (by_count ? at >= bp && at < bp + c : at >= bw && at < bw + w) {
@@ -442,11 +458,11 @@ __device__ __forceinline__ bool narrow(Shared& sh, const Row<kThreads>& row, con
     lo = hi - lo < width ? lo : hi - width;
     __syncthreads();
   }
-  if (held <= kSmall) {
+  if (held <= NT) {
     __syncthreads();
     if (tid == 0) sh.n_small = 0;
     __syncthreads();
-    row.each<8>([&](float l, int j) {
+    row.template each<8>([&](float l, int j) {
       const uint32_t k = key_of(l);
       if (k >= lo && k <= hi) sh.small[atomicAdd(&sh.n_small, 1u)].x = entry_of(k, j);
     });
@@ -454,17 +470,17 @@ __device__ __forceinline__ bool narrow(Shared& sh, const Row<kThreads>& row, con
     return true;
   }
   // Equal logits, as many as there are: the place among them in order of the index.
-  // The indices are cut into kSub parts in the same way.
+  // The indices are cut into NT parts in the same way.
   const uint64_t w = sc.weight(logit_of(lo));
   const uint64_t want = by_count ? at - place : (at - before) / w;
   uint32_t first = 0, span = static_cast<uint32_t>(row.n);
   uint64_t skipped = 0;
   while (span > 1) {
-    const uint32_t part = (span + kSub - 1) / kSub;
+    const uint32_t part = (span + NT - 1) / NT;
     __syncthreads();
     sh.sub_c[tid] = 0;
     __syncthreads();
-    row.each<8>([&](float l, int j) {
+    row.template each<8>([&](float l, int j) {
       const uint32_t at_j = static_cast<uint32_t>(j) - first;
       if (at_j < span && key_of(l) == lo) atomicAdd(&sh.sub_c[at_j / part], 1u);
     });
@@ -476,7 +492,7 @@ __device__ __forceinline__ bool narrow(Shared& sh, const Row<kThreads>& row, con
     }
     if ((tid & 63) == 63) sh.wave_c[tid >> 6] = upto;
     __syncthreads();
-    upto += waves_before(sh.wave_c);
+    upto += waves_before<NT>(sh.wave_c);
     const uint64_t b = skipped + upto - c;
     if (want >= b && want < b + c) {
       sh.found_bucket = tid;
@@ -493,13 +509,13 @@ __device__ __forceinline__ bool narrow(Shared& sh, const Row<kThreads>& row, con
 }
 
 // The tokens that `in` takes into the list, as far as they fit; sh.n_list counts them.
-template <class In>
-__device__ __forceinline__ void collect(Shared& sh, const Row<kThreads>& row, In in) {
+template <int NT, class In>
+__device__ __forceinline__ void collect(Shared& sh, const Row<NT>& row, In in) {
   // An address the compiler takes for a lane's own: LDS adds the lanes' counts one
   // after the other faster than the scan that it would put in their place.
   uint32_t own = 0;
   asm volatile("" : "+v"(own));
-  row.each4<4>([&](const float (&x)[4], int j, int count) {
+  row.template each4<4>([&](const float (&x)[4], int j, int count) {
     uint32_t taken = 0;
 #pragma unroll
     for (int k = 0; k < 4; ++k) taken += k < count && in(x[k]);
@@ -520,11 +536,12 @@ __device__ __forceinline__ void collect(Shared& sh, const Row<kThreads>& row, In
 // already, together with what the searches that follow are known to want: with
 // `reach`, all buckets before it, if they fit, else those that hold share * W for the
 // weights W that may yet turn out to be kept (of `bucket` and `near`).
-__device__ Found locate(Shared& sh, const Row<kThreads>& row, const Scale& sc, bool by_count,
+template <int NT>
+__device__ Found locate(Shared& sh, const Row<NT>& row, const Scale& sc, bool by_count,
                         uint64_t at, bool counted, bool reach, double share, uint64_t near,
                         Listed& listed) {
   const int tid = threadIdx.x;
-  const int bucket = part_of(sh, sh.before, sh.places, kBuckets, by_count, at);
+  const int bucket = part_of<NT>(sh, by_count, at);
   uint64_t before = sh.before[bucket];
   uint64_t place = counted ? sh.places[bucket] : 0;
   bool many = false;
@@ -538,10 +555,10 @@ __device__ Found locate(Shared& sh, const Row<kThreads>& row, const Scale& sc, b
       const double least = share * static_cast<double>(before < near ? before : near);
       const double most = share * static_cast<double>(after < near ? after : near);
       const uint64_t first = static_cast<uint64_t>(least);
-      const int lo2 = part_of(sh, sh.before, sh.places, kBuckets, false,
+      const int lo2 = part_of<NT>(sh, false,
                               first < after ? first : after - 1);
       const uint64_t last = static_cast<uint64_t>(most);
-      const int hi2 = part_of(sh, sh.before, sh.places, kBuckets, false,
+      const int hi2 = part_of<NT>(sh, false,
                               last < after ? last : after - 1);
       listed.lo2 = lo2;
       listed.hi2 = hi2 < bucket ? hi2 : bucket - 1;
@@ -562,23 +579,23 @@ __device__ Found locate(Shared& sh, const Row<kThreads>& row, const Scale& sc, b
   if (!many) {  // the bucket's own among the collected
     if (tid == 0) sh.n_small = 0;
     __syncthreads();
-    for (uint32_t i = tid; i < listed.n; i += kThreads) {
+    for (uint32_t i = tid; i < listed.n; i += NT) {
       const uint64_t e = sh.list[i];
       if (sc.bucket(logit_of(static_cast<uint32_t>(e >> 32))) == bucket) {
         const uint32_t k = atomicAdd(&sh.n_small, 1u);
-        if (k < kSmall) sh.small[k].x = e;
+        if (k < NT) sh.small[k].x = e;
       }
     }
     __syncthreads();
-    many = sh.n_small > kSmall;
+    many = sh.n_small > NT;
   }
   if (many) {
     __syncthreads();
     listed = {0, -1, 0, -1, 0};
     Found f;
-    if (!narrow(sh, row, sc, bucket, by_count, at, before, place, f)) return f;
+    if (!narrow<NT>(sh, row, sc, bucket, by_count, at, before, place, f)) return f;
   }
-  return among_small(sh, sc, by_count, at, before, place);
+  return among_small<NT>(sh, sc, by_count, at, before, place);
 }
 
 // A row's parameters.
@@ -665,12 +682,13 @@ __device__ uint64_t weigh(Weights& sh, double* table, const Row<NT>& row, const 
 }
 
 // The rest: from a row's weights, the filters' ends and the draw.
+template <int NT>
 __device__ void pick(const SampleArgs& a, Shared& sh, int64_t r, const Params& p, const Scale& sc,
                      uint64_t near) {
   const int tid = threadIdx.x;
-  const Row<kThreads> row = {a.L + r * a.ldl, static_cast<int>(a.vocab)};
+  const Row<NT> row = {a.L + r * a.ldl, static_cast<int>(a.vocab)};
   const bool use_k = p.use_k(a.vocab), use_p = p.use_p(), counted = p.counted(a.vocab);
-  running(sh, sh.before, sh.places, kBuckets);
+  running<NT>(sh);
   if (tid == 0) sh.places[kBuckets] = static_cast<uint32_t>(a.vocab);  // with those of no weight
   uint64_t kept = sh.before[kBuckets];
   __syncthreads();
@@ -691,7 +709,7 @@ __device__ void pick(const SampleArgs& a, Shared& sh, int64_t r, const Params& p
       at = static_cast<uint64_t>(p.share() * static_cast<double>(kept));
     }
     if (stage > 0) at = at < kept - 1 ? at : kept - 1;
-    const Found f = locate(sh, row, sc, stage == 0, at, counted, stage < 2, p.share(),
+    const Found f = locate<NT>(sh, row, sc, stage == 0, at, counted, stage < 2, p.share(),
                            p.use_m() ? near : ~uint64_t(0), listed);
     if (stage < 2) {
       kept = f.before + f.w;
@@ -705,22 +723,23 @@ __device__ void pick(const SampleArgs& a, Shared& sh, int64_t r, const Params& p
 
 // A row that needs no weights, given its largest logit: one without a token, one
 // with a NaN, or the first of the largest logits.
+template <int NT>
 __device__ bool pick_plain(const SampleArgs& a, uint32_t* wave_c, int64_t r, const Params& p,
                            float m) {
   int32_t token = -1;
   float prob = m != m ? m : 0.0f;
   if (m > -__builtin_inff()) {
     if (!p.greedy()) return false;
-    const Row<kThreads> row = {a.L + r * a.ldl, static_cast<int>(a.vocab)};
+    const Row<NT> row = {a.L + r * a.ldl, static_cast<int>(a.vocab)};
     uint32_t first = 0xffffffffu;
-    row.each4<4>([&](const float (&x)[4], int j, int count) {
+    row.template each4<4>([&](const float (&x)[4], int j, int count) {
 #pragma unroll
       for (int k = 3; k >= 0; --k) {  // (j grows from one call to the next)
         const uint32_t at = static_cast<uint32_t>(j + k);
         if (x[k] == m && k < count && at < first) first = at;
       }
     });
-    token = static_cast<int32_t>(block_reduce<kThreads>(
+    token = static_cast<int32_t>(block_reduce<NT>(
         first, wave_c, [](uint32_t x, uint32_t y) { return x < y ? x : y; }));
     prob = 1.0f;
   }
@@ -736,16 +755,17 @@ __device__ __forceinline__ Scale scale_of(const Params& p, float m) {
 }
 
 // One workgroup a row.
-__global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
+template <int NT>
+__global__ __launch_bounds__(NT, 4) void sample_kernel(SampleArgs a) {
   __shared__ Shared sh;
   const int64_t r = blockIdx.x;
-  const Row<kThreads> row = {a.L + r * a.ldl, static_cast<int>(a.vocab)};
+  const Row<NT> row = {a.L + r * a.ldl, static_cast<int>(a.vocab)};
   const Params p(a, r);
   const float m = find_top(row, sh.wave_m);
-  if (pick_plain(a, sh.wave_c, r, p, m)) return;
+  if (pick_plain<NT>(a, sh.wave_c, r, p, m)) return;
   const Scale sc = scale_of(p, m);
   const uint64_t near = weigh(sh, sh.table, row, p, sc, p.counted(a.vocab));
-  pick(a, sh, r, p, sc, near);
+  pick<NT>(a, sh, r, p, sc, near);
 }
 
 // Long rows: a stretch of `stretch` tokens of a row per workgroup in the first two
@@ -821,7 +841,7 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(SampleArgs a, con
   const Part* part = parts + r * G;
   const Params p(a, r);
   const float m = top_of(part, G);
-  if (pick_plain(a, sh.wave_c, r, p, m)) return;
+  if (pick_plain<kThreads>(a, sh.wave_c, r, p, m)) return;
   const bool counted = p.counted(a.vocab);
   for (int b = threadIdx.x; b < kBuckets; b += kThreads) {
     sh.before[b] = sum_parts(part, G, [&](const Part& q) { return q.weight[b]; });
@@ -829,7 +849,7 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(SampleArgs a, con
   }
   const uint64_t near = p.use_m() ? sum_parts(part, G, [](const Part& q) { return q.near; }) : 0;
   __syncthreads();
-  pick(a, sh, r, p, scale_of(p, m), near);
+  pick<kThreads>(a, sh, r, p, scale_of(p, m), near);
 }
 
 // How long rows are cut up.
@@ -891,7 +911,14 @@ hipError_t launch_sample(const SampleArgs& a, void* workspace, hipStream_t s) {
     if (a.prob) g.prob = a.prob + r0;
     const dim3 wide(static_cast<unsigned>(g.rows * p.G)), rows(static_cast<unsigned>(g.rows));
     if (one) {
-      hipLaunchKernelGGL(sample_kernel, rows, dim3(kThreads), 0, s, g);
+      // Of more rows than compute units, two workgroups a unit that run into each
+      // other's gaps (512 x 131072: 140 us against 149, 1000 x 1000: 18.5 against 34; 256
+      // rows and fewer are walked faster by 1024 threads), unless rows are so long that
+      // buckets of more than 512 tokens are the rule (300 x 500000: 726 against 622).
+      if (a.rows > 256 && a.vocab <= 262144)
+        hipLaunchKernelGGL(sample_kernel<512>, rows, dim3(512), 0, s, g);
+      else
+        hipLaunchKernelGGL(sample_kernel<1024>, rows, dim3(1024), 0, s, g);
     } else {
       hipLaunchKernelGGL(sample_top_kernel, wide, dim3(kWeighThreads), 0, s, g, parts, p.G,
                          p.stretch);

@@ -414,6 +414,24 @@ def test_sample_rows_equal_and_special_logits(rp, vocab):
     check_draw(rp, L, np.resize(np.array([nan, -1, 1, 2, inf, -inf], np.float32), n), "odd u")
 
 
+@pytest.mark.parametrize("vocab,std", [(1, 1), (130, 2.5), (777, 2.5), (20011, 2.5), (20011, 0.01),
+                                       (60013, 0.3)])
+def test_sample_rows_of_many_rows(rp, vocab, std):
+    """More rows than compute units, wide and narrow (one bucket may hold them all),
+    every filter in turn."""
+    rows = 260
+    L, u = draw_inputs(2250 + vocab, rows, vocab, std=std, peaks=0 if std < 1 else 4)
+    L[::7] = np.rint(L[::7] * np.float32(8 / std)) * np.float32(std / 8)  # equal logits
+    L[3::11, ::3] = -np.inf
+    g = inputs.rng(2260 + vocab)
+    pick = lambda *v: g.choice(np.array(v), rows)  # noqa: E731
+    check_draw(rp, L, u, "many rows")
+    check_draw(rp, L, u, "many rows filters", temperature=pick(0, 1, 0.3, 5, 1e30).astype(np.float32),
+               top_k=pick(0, 1, 40, 3000, vocab).astype(np.int32),
+               top_p=pick(1, 0.5, 0, 0.99).astype(np.float32),
+               min_p=pick(0, 0.1, 1, 0.001).astype(np.float32))
+
+
 @pytest.mark.parametrize("ranked", [False, True])
 def test_sample_rows_against_64_bits(rp, ranked):
     """A draw's place in the plain 64-bit distribution: each weight is off by at
