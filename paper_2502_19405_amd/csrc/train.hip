@@ -773,8 +773,11 @@ __device__ __forceinline__ void layernorm_bwd_rows_grouped(const RowBwdArgs& a, 
 // lane; wider rows (up to 64 values per lane) shared by four waves of 16
 // values each, which leaves the registers for two workgroups per compute unit
 // (measured faster than one wave of 64 or two of 32; for 32 values per lane
-// one wave measured faster than two of 16).
-constexpr int kColsplitGroupT = 16;
+// one wave measured faster than two of 16).  With dS's values as well, eight
+// waves of 8 values and from 32 values per lane four (4096 x 4096: 58 us
+// against 68 with 16 values; without dS 50 against 48.7).
+constexpr int colsplit_alone(int add) { return add ? 16 : 32; }
+constexpr int colsplit_group(int add) { return add ? 8 : 16; }
 
 template <int T, int SWU, int ADD>
 __global__ __launch_bounds__(kSplitWaves * kWave) void layernorm_bwd_colsplit_kernel(
@@ -829,12 +832,10 @@ __global__ __launch_bounds__(kSplitWaves * kWave) void layernorm_bwd_colsplit_ke
   // find it in L2.  (A chunk's dX just before its chains, which brings the
   // two reads together, measured slower: each chunk then waits for its own
   // rows.)
-  if constexpr (T > 32) {
-    static_assert(T % kColsplitGroupT == 0 && kSplitWaves % (T / kColsplitGroupT) == 0,
-                  "row groups must tile the workgroup");
-    constexpr int S = T / kColsplitGroupT, P = kSplitWaves / S;
-    layernorm_bwd_rows_grouped<kColsplitGroupT, S, ADD>(a, r0 + int64_t(g) * P, int64_t(P) * G, r1,
-                                                        lane, w);
+  if constexpr (T > colsplit_alone(ADD)) {
+    constexpr int own = colsplit_group(ADD), S = T / own, P = kSplitWaves / S;
+    static_assert(T % own == 0 && kSplitWaves % S == 0, "row groups must tile the workgroup");
+    layernorm_bwd_rows_grouped<own, S, ADD>(a, r0 + int64_t(g) * P, int64_t(P) * G, r1, lane, w);
   } else {
     const int64_t stride = int64_t(kSplitWaves) * G;
     for (int64_t row = r0 + int64_t(g) * kSplitWaves + w; row < r1; row += stride)
