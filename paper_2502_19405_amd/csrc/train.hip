@@ -776,7 +776,7 @@ __device__ __forceinline__ void layernorm_bwd_rows_grouped(const RowBwdArgs& a, 
 // one wave measured faster than two of 16).  With dS's values as well, eight
 // waves of 8 values and from 32 values per lane four (4096 x 4096: 58 us
 // against 68 with 16 values; without dS 50 against 48.7).
-constexpr int colsplit_alone(int add) { return add ? 16 : 32; }
+constexpr int colsplit_alone(int add) { return add ? 12 : 32; }
 constexpr int colsplit_group(int add) { return add ? 8 : 16; }
 
 template <int T, int SWU, int ADD>
