@@ -774,8 +774,9 @@ __device__ __forceinline__ void layernorm_bwd_rows_grouped(const RowBwdArgs& a, 
 // values each, which leaves the registers for two workgroups per compute unit
 // (measured faster than one wave of 64 or two of 32; for 32 values per lane
 // one wave measured faster than two of 16).  With dS's values as well, eight
-// waves of 8 values and from 32 values per lane four (4096 x 4096: 58 us
-// against 68 with 16 values; without dS 50 against 48.7).
+// waves of 8 values, and four or two from 16 values per lane on (4096 x 4096:
+// 59 us against 68 with 16 values; 1531 x 1001: 12.1 against 14.8 by one wave;
+// without dS groups of 8 take 50 us at 4096 x 4096 against 48.7).
 constexpr int colsplit_alone(int add) { return add ? 12 : 32; }
 constexpr int colsplit_group(int add) { return add ? 8 : 16; }
 

@@ -893,6 +893,10 @@ def _row_major(t: torch.Tensor, name: str):
     return _rows(t, name)
 
 
+def _like(X: torch.Tensor) -> torch.Tensor:
+    return torch.empty_like(X, memory_format=torch.contiguous_format)
+
+
 def _matrix(t, shape, dtype, device: int, name: str):
     """(address, row stride) of an optional matrix of this shape."""
     if t is None:
@@ -954,9 +958,9 @@ def add_rmsnorm_rows(X: torch.Tensor, R: torch.Tensor | None = None,
     and out may each be X or R."""
     ldx = _row_major(X, "X")[2]
     if sum_out is None and R is not None:
-        sum_out = X.new_empty(X.shape)
+        sum_out = _like(X)
     if out is None:
-        out = X.new_empty(X.shape)
+        out = _like(X)
     _add_rmsnorm(X, ldx, X.get_device(), R, gamma, eps, order, launch, sum_out, out, None, None,
                  rstd_out)
     return X if sum_out is None else sum_out, out
@@ -974,7 +978,7 @@ def add_rmsnorm_quantize_rows(X: torch.Tensor, R: torch.Tensor | None = None,
     scales of the Y it gives, which is written only if out is passed."""
     rows, _, ldx = _row_major(X, "X")
     if sum_out is None and R is not None:
-        sum_out = X.new_empty(X.shape)
+        sum_out = _like(X)
     if q_out is None:
         q_out = X.new_empty(X.shape, dtype=_I8)
     if scale_out is None:
@@ -999,7 +1003,7 @@ def add_rmsnorm_backward_rows(S: torch.Tensor, dY: torch.Tensor, rstd: torch.Ten
     dx = dgamma = None
     wptr, wbytes = None, 0
     if need_dx:
-        dx = dx_out if dx_out is not None else S.new_empty(shape)
+        dx = dx_out if dx_out is not None else _like(S)
     if need_dgamma:
         dgamma = dgamma_out if dgamma_out is not None else S.new_empty(cols)
         if workspace is None:

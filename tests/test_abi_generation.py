@@ -201,6 +201,10 @@ class Meta:
     def new_empty(self, *a, **k):
         return Meta(self.t.new_empty(*a, **k), self.device_index)
 
+    @classmethod
+    def __torch_function__(cls, func, types, args=(), kwargs=None):
+        return Meta(func(args[0].t, *args[1:], **(kwargs or {})), args[0].device_index)
+
 
 def test_binding_checks_shapes_types_and_devices():
     f, i8 = torch.float32, torch.int8
