@@ -29,6 +29,10 @@ typedef __attribute__((address_space(1))) void* global_void_ptr;
 
 constexpr int kChunk = 16;  // codes in one lane's operand
 
+// How operands are read: 16 codes at a time straight to LDS (aligned), through
+// registers, or byte by byte (k below 16).
+enum { kDirect, kStaged, kShort };
+
 template <int N>
 __device__ __forceinline__ void wait_vmcnt() {
   static_assert(N >= 0 && N < 64, "vmcnt range");
@@ -41,17 +45,37 @@ __device__ __forceinline__ float q8_output(int acc, float sa, float sb) {
   return c * sb;
 }
 
-// 16 codes of a row from index kk on, +0 past K (kk may be past it).
-__device__ __forceinline__ v4i load_codes(const int8_t* row, int64_t kk, int64_t K) {
+// 16 codes of a row from index kk on, +0 past K (kk may be past it), in two steps: the
+// load, which never reads past K, and the move to their places.  SHORT: K below 16,
+// single bytes are read.
+template <bool SHORT>
+__device__ __forceinline__ v4i load_raw(const int8_t* row, int kk, int K) {
   v4i v = {0, 0, 0, 0};
-  if (kk + kChunk <= K) {
-    __builtin_memcpy(&v, row + kk, kChunk);  // any alignment
-  } else {
+  if constexpr (SHORT) {
 #pragma unroll
     for (int b = 0; b < kChunk; ++b)
-      if (kk + b < K) v[b / 4] |= static_cast<int>(static_cast<uint8_t>(row[kk + b])) << (8 * (b % 4));
+      if (b < K) v[b / 4] |= static_cast<int>(static_cast<uint8_t>(row[b])) << (8 * (b % 4));
+  } else {
+    __builtin_memcpy(&v, row + (kk + kChunk <= K ? kk : K - kChunk), kChunk);  // any alignment
   }
   return v;
+}
+__device__ __forceinline__ v4i placed(v4i v, int kk, int K) {
+  // bytes before kk that the load began with
+  const int over = K >= kChunk ? kk + kChunk - K : kk;
+  if (over <= 0) return v;
+  uint64_t lo = static_cast<uint32_t>(v[0]) | static_cast<uint64_t>(static_cast<uint32_t>(v[1])) << 32;
+  uint64_t hi = static_cast<uint32_t>(v[2]) | static_cast<uint64_t>(static_cast<uint32_t>(v[3])) << 32;
+  const int bits = over * 8;
+  if (bits < 64) {
+    lo = lo >> bits | hi << (64 - bits);
+    hi = hi >> bits;
+  } else {
+    lo = bits < 128 ? hi >> (bits - 64) : 0;
+    hi = 0;
+  }
+  return v4i{static_cast<int>(lo), static_cast<int>(lo >> 32), static_cast<int>(hi),
+             static_cast<int>(hi >> 32)};
 }
 
 // ---------------------------------------------------------------------------
@@ -226,46 +250,69 @@ struct Q8Tile {
     __syncthreads();
   }
 
-  // Any alignment and any K: slices through registers into a pair of slots.
+  // Any alignment and any K: slices through registers into a pair of slots, the loads
+  // of two slices in flight where there are the registers (not the 256 x 256 tile's).
+  template <bool SHORT>
   __device__ static void run_any(const Q8Args& g, Smem& sm, int64_t m0, int64_t n0, int wave,
                                  int lane, const Reads& rd, v16i (&acc)[IM][IN]) {
     static_assert(NS == 2, "a pair of slots");
     const int K = static_cast<int>(g.k);
     const int nslices = (K + BK - 1) / BK;
     const Src src = sources(g, m0, n0, wave, lane);
-    v4i ra[AU], rb[BU];
-    auto fetch = [&](int s) {
-#pragma unroll
-      for (int u = 0; u < AU; ++u) ra[u] = load_codes(src.a[u], s * BK + src.ka[u], K);
-#pragma unroll
-      for (int u = 0; u < BU; ++u) rb[u] = load_codes(src.b[u], s * BK + src.kb[u], K);
+    struct Staged {
+      v4i a[AU], b[BU];
     };
-    auto put = [&](int slot) {
+    Staged even, odd;
+    if (nslices == 0) return;
+    // (no conditions round the loads and stores, which would have the waits between them
+    // wait for all: the last slice again past the end, its slot not read)
+    auto fetch = [&](Staged& r, int s) {
+      s = s < nslices ? s : nslices - 1;
+#pragma unroll
+      for (int u = 0; u < AU; ++u) r.a[u] = load_raw<SHORT>(src.a[u], s * BK + src.ka[u], K);
+#pragma unroll
+      for (int u = 0; u < BU; ++u) r.b[u] = load_raw<SHORT>(src.b[u], s * BK + src.kb[u], K);
+    };
+    auto put = [&](Staged& r, int s) {
+      if ((s + 1) * BK > K) {
+#pragma unroll
+        for (int u = 0; u < AU; ++u) r.a[u] = placed(r.a[u], s * BK + src.ka[u], K);
+#pragma unroll
+        for (int u = 0; u < BU; ++u) r.b[u] = placed(r.b[u], s * BK + src.kb[u], K);
+      }
 #pragma unroll
       for (int u = 0; u < AU; ++u)
-        *reinterpret_cast<v4i*>(sm.a[slot] + (wave + u * NW) * 1024 + lane * kChunk) = ra[u];
+        *reinterpret_cast<v4i*>(sm.a[s & 1] + (wave + u * NW) * 1024 + lane * kChunk) = r.a[u];
 #pragma unroll
       for (int u = 0; u < BU; ++u)
-        *reinterpret_cast<v4i*>(sm.b[slot] + (wave + u * NW) * 1024 + lane * kChunk) = rb[u];
+        *reinterpret_cast<v4i*>(sm.b[s & 1] + (wave + u * NW) * 1024 + lane * kChunk) = r.b[u];
     };
-    if (nslices > 0) {
-      fetch(0);
-      put(0);
-    }
-    __syncthreads();
-    for (int s = 0; s < nslices; ++s) {
-      const int slot = s & 1;
-      if (s + 1 < nslices) fetch(s + 1);
+    constexpr int kAhead = BM * BN <= 128 * 128 ? 2 : 1;
+    // mine: slice s, in its slot by now; next: slice s + 1, to be put there
+    auto turn = [&](Staged& mine, Staged& next, int s) {
+      fetch(mine, s + kAhead);
 #pragma unroll
       for (int q = 0; q < STEPS; ++q) {
         Pack pk;
 #pragma unroll
-        for (int r = 0; r < IM + IN; ++r) read_one(sm.a[slot], sm.b[slot], rd, q, r, pk);
+        for (int r = 0; r < IM + IN; ++r) read_one(sm.a[s & 1], sm.b[s & 1], rd, q, r, pk);
 #pragma unroll
         for (int t = 0; t < IM * IN; ++t) step(pk, t, acc);
       }
-      if (s + 1 < nslices) put(slot ^ 1);  // its last readers are behind the barrier below
+      put(next, s + 1);  // its slot's last readers are behind the barrier of the turn before
       __syncthreads();
+    };
+    fetch(even, 0);
+    if constexpr (kAhead == 2) fetch(odd, 1);
+    put(even, 0);
+    __syncthreads();
+    if constexpr (kAhead == 2) {
+      for (int s = 0; s < nslices; s += 2) {
+        turn(even, odd, s);
+        if (s + 1 < nslices) turn(odd, even, s + 1);
+      }
+    } else {
+      for (int s = 0; s < nslices; ++s) turn(even, even, s);
     }
   }
 
@@ -346,7 +393,7 @@ __device__ __forceinline__ bool locate(int64_t tiles_m, int64_t tiles_n, int64_t
   return true;
 }
 
-template <int BM, int BN, int WM, int WN, int BK, int NS, bool ANY>
+template <int BM, int BN, int WM, int WN, int BK, int NS, int LOADS>
 __global__ __launch_bounds__(WM* WN * 64) void q8_tile_kernel(Q8Args g, int64_t tiles_m,
                                                               int64_t tiles_n, int64_t per) {
   using Tile = Q8Tile<BM, BN, WM, WN, BK, NS>;
@@ -362,7 +409,8 @@ __global__ __launch_bounds__(WM* WN * 64) void q8_tile_kernel(Q8Args g, int64_t 
   for (int i = 0; i < Tile::IM; ++i)
 #pragma unroll
     for (int j = 0; j < Tile::IN; ++j) acc[i][j] = v16i{};
-  if constexpr (ANY) Tile::run_any(g, sm, tm * BM, tn * BN, wave, lane, rd, acc);
+  if constexpr (LOADS != kDirect)
+    Tile::template run_any<LOADS == kShort>(g, sm, tm * BM, tn * BN, wave, lane, rd, acc);
   else Tile::run(g, sm, tm * BM, tn * BN, wave, lane, rd, acc);
   const int64_t m0 = tm * BM + wm0, n0 = tn * BN + wn0;
   if (m0 + Tile::TM <= g.m && n0 + Tile::TN <= g.n)
@@ -372,32 +420,33 @@ __global__ __launch_bounds__(WM* WN * 64) void q8_tile_kernel(Q8Args g, int64_t 
 }
 
 // ---------------------------------------------------------------------------
-// Few rows: bound by reading B.  A workgroup owns 16 columns and MT tiles of 16
-// rows; its waves share the contraction, 128 codes each in turn (a whole line of
+// Few rows, or few outputs with long sums: bound by reading B.  A workgroup owns 16
+// columns and MT tiles of 16 rows; its waves share the contraction, 128 codes each in turn (a whole line of
 // every row), and the sums meet in LDS.  Operands go from global
 // memory to registers; the lanes of rows past the last one load nothing.
 // ---------------------------------------------------------------------------
 
 constexpr int kFewWaves = 8;
 
-template <int MT>
+template <int MT, bool SHORT>
 __global__ __launch_bounds__(kFewWaves * 64) void q8_few_kernel(Q8Args g) {
   __shared__ int part[kFewWaves][MT * 256];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r16 = lane & 15, quarter = lane >> 4;
-  const int64_t K = g.k;
+  const int64_t K = g.k, m0 = static_cast<int64_t>(blockIdx.y) * (MT * 16);
   const int8_t* a[MT];
   bool live[MT];
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
-    live[t] = t * 16 + r16 < g.m;
-    a[t] = g.A + (live[t] ? t * 16 + r16 : 0) * g.lda + quarter * 32;
+    const int64_t i = m0 + t * 16 + r16;
+    live[t] = i < g.m;
+    a[t] = g.A + (live[t] ? i : 0) * g.lda;
   }
   for (int64_t n0 = static_cast<int64_t>(blockIdx.x) * 16; n0 < g.n;
        n0 += static_cast<int64_t>(gridDim.x) * 16) {
     const int64_t j = n0 + r16;
-    const int8_t* b = g.B + (j < g.n ? j : g.n - 1) * g.ldb + quarter * 32;
+    const int8_t* b = g.B + (j < g.n ? j : g.n - 1) * g.ldb;
     v4i acc[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t) acc[t] = v4i{0, 0, 0, 0};
@@ -412,7 +461,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void q8_few_kernel(Q8Args g) {
       for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-          __builtin_memcpy(&bv[u][h], b + k0 + u * kStep + h * kChunk, kChunk);
+          __builtin_memcpy(&bv[u][h], b + k0 + quarter * 32 + u * kStep + h * kChunk, kChunk);
 #pragma unroll
       for (int t = 0; t < MT; ++t) {
 #pragma unroll
@@ -424,7 +473,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void q8_few_kernel(Q8Args g) {
           for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-              __builtin_memcpy(&av[u][h][t], a[t] + k0 + u * kStep + h * kChunk, kChunk);
+              __builtin_memcpy(&av[u][h][t], a[t] + k0 + quarter * 32 + u * kStep + h * kChunk, kChunk);
         }
       }
 #pragma unroll
@@ -436,14 +485,22 @@ __global__ __launch_bounds__(kFewWaves * 64) void q8_few_kernel(Q8Args g) {
             acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(av[u][h][t], bv[u][h], acc[t], 0, 0, 0);
     }
     for (; k0 < K; k0 += kStep) {
+      const int at = static_cast<int>(k0) + quarter * 32, end = static_cast<int>(K);
+      v4i bv[2], av[2][MT];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int64_t kk = k0 + h * kChunk, end = K - quarter * 32;
-        const v4i bv = load_codes(b, kk, end);
+        bv[h] = load_raw<SHORT>(b, at + h * kChunk, end);
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
-          acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(
-              live[t] ? load_codes(a[t], kk, end) : v4i{0, 0, 0, 0}, bv, acc[t], 0, 0, 0);
+        for (int t = 0; t < MT; ++t) av[h][t] = load_raw<SHORT>(a[t], at + h * kChunk, end);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const v4i bp = placed(bv[h], at + h * kChunk, end);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+          const v4i ap = live[t] ? placed(av[h][t], at + h * kChunk, end) : v4i{0, 0, 0, 0};
+          acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(ap, bp, acc[t], 0, 0, 0);
+        }
       }
     }
     // element r of a lane: row 4 (lane / 16) + r, column lane % 16
@@ -453,7 +510,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void q8_few_kernel(Q8Args g) {
       for (int r = 0; r < 4; ++r) part[wave][(t * 16 + quarter * 4 + r) * 16 + r16] = acc[t][r];
     __syncthreads();
     for (int o = threadIdx.x; o < MT * 256; o += kFewWaves * 64) {
-      const int64_t row = o / 16, col = n0 + o % 16;
+      const int64_t row = m0 + o / 16, col = n0 + o % 16;
       if (row >= g.m || col >= g.n) continue;
       int sum = 0;
 #pragma unroll
@@ -468,17 +525,20 @@ __global__ __launch_bounds__(kFewWaves * 64) void q8_few_kernel(Q8Args g) {
 template <int MT>
 hipError_t launch_few(const Q8Args& g, hipStream_t s) {
   const int64_t groups = (g.n + 16 - 1) / 16, cap = int64_t(1) << 22;
-  hipLaunchKernelGGL(q8_few_kernel<MT>, dim3(static_cast<unsigned>(groups < cap ? groups : cap)),
+  const int64_t blocks = (g.m + MT * 16 - 1) / (MT * 16);
+  hipLaunchKernelGGL((g.k < kChunk ? q8_few_kernel<MT, true> : q8_few_kernel<MT, false>),
+                     dim3(static_cast<unsigned>(groups < cap ? groups : cap),
+                          static_cast<unsigned>(blocks)),
                      dim3(kFewWaves * 64), 0, s, g);
   return hipGetLastError();
 }
 
-template <int BM, int BN, int WM, int WN, int BK, int NS, bool ANY>
+template <int BM, int BN, int WM, int WN, int BK, int NS, int LOADS>
 hipError_t launch_tiles(const Q8Args& g, hipStream_t s) {
   const int64_t tm = (g.m + BM - 1) / BM, tn = (g.n + BN - 1) / BN;
   const int64_t per = (tm * tn + 7) / 8;
   if (per * 8 > max_workgroups(WM * WN * 64)) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((q8_tile_kernel<BM, BN, WM, WN, BK, NS, ANY>),
+  hipLaunchKernelGGL((q8_tile_kernel<BM, BN, WM, WN, BK, NS, LOADS>),
                      dim3(static_cast<unsigned>(per * 8)), dim3(WM * WN * 64), 0, s, g, tm, tn, per);
   return hipGetLastError();
 }
@@ -489,30 +549,42 @@ hipError_t launch_matmul_q8(const Q8Args& g, hipStream_t s) {
   const bool direct = g.k > 0 && g.k % kChunk == 0 && g.lda % kChunk == 0 && g.ldb % kChunk == 0 &&
                       reinterpret_cast<uintptr_t>(g.A) % kChunk == 0 &&
                       reinterpret_cast<uintptr_t>(g.B) % kChunk == 0;
-  // Up to 8 rows, and up to 32 with few columns, where tiles are too few to read B
-  // with (4 x 32000, k 4096: 27.9 us against 31.2 with 64 x 64 tiles; 32 x 4096, k
-  // 14336: 25 against 32; but 32 x 14336, k 4096: 29 against 15.6, and 16 rows 18.2 against 15.2).
-  if (g.m <= 8) return launch_few<1>(g, s);
-  if (g.m <= 32 && g.n < 8192) return g.m <= 16 ? launch_few<1>(g, s) : launch_few<2>(g, s);
-  // Otherwise the tiles with the smallest estimate: rounds over the compute units
-  // times slices times what a slice of such a tile takes a compute unit, measured
-  // with 4096 and 14336 columns (225, 640 and 1970 ns; the larger a tile, the fewer of its operands are loaded twice).
-  // Up to one 128 x 128 tile a unit, a deeper ring of slices makes up for the
-  // second workgroup (256 x 14336, k 4096: 27 us against 35).
+  // Tiles by their estimate: rounds over the compute units times slices times what a
+  // slice of such a tile takes a compute unit, measured with 4096 and 14336 columns (225,
+  // 640 and 1970 ns; the larger a tile, the fewer of its operands are loaded twice;
+  // through registers 1.4 times that: 333 x 1001, k 3000: 10.5 us).  Up to one 128 x 128
+  // tile a unit, a deeper ring of slices makes up for the second workgroup (256 x
+  // 14336, k 4096: 27 us against 35).
   const int64_t cus = device_cus() > 0 ? device_cus() : 256;
   auto tiles = [&](int64_t edge) { return ((g.m + edge - 1) / edge) * ((g.n + edge - 1) / edge); };
   auto cost = [&](int64_t edge, int64_t ns) { return (tiles(edge) + cus - 1) / cus * ns; };
   const int64_t small = cost(64, 225), middle = cost(128, 640), large = cost(256, 1970);
+  const int64_t least = small < middle ? (small < large ? small : large)
+                                       : (middle < large ? middle : large);
+  // The kernel for few rows, where tiles are too few to fill the card or their slices too
+  // many: its workgroups read 32 or 48 rows of codes for 256 or 512 outputs, at 8 bytes
+  // a ns over the card, half that without alignment (4 x 32000, k 4096: 27.9 us against
+  // 31.2 by tiles; 32 x 4096, k 14336: 25 and 32; 64 x 1024, k 4096: 7.1 and 10.1; 40 x
+  // 200, k 5000: 7.0 and 22.3; but 32 x 14336, k 4096: 29 and 15.6; 64 x 4096, k 4096:
+  // 14.2 and 10.3).
+  const int64_t mt = g.m <= 16 ? 1 : 2, blocks = (g.m + 16 * mt - 1) / (16 * mt);
+  const double few = static_cast<double>(blocks) * static_cast<double>((g.n + 15) / 16) *
+                     static_cast<double>(g.k) * (mt == 1 ? 0.0039 : 0.0058) * (direct ? 1 : 2);
+  const double tiled = static_cast<double>(least) * static_cast<double>((g.k + 127) / 128) *
+                       (direct ? 1 : 1.4);
+  if (g.m <= 8 || (few < tiled && blocks <= 65535))
+    return mt == 1 ? launch_few<1>(g, s) : launch_few<2>(g, s);
+  if (g.k < kChunk) return launch_tiles<64, 64, 2, 2, 128, 2, kShort>(g, s);
   if (large <= middle && large <= small)
-    return direct ? launch_tiles<256, 256, 2, 4, 128, 2, false>(g, s)
-                  : launch_tiles<256, 256, 2, 4, 128, 2, true>(g, s);
+    return direct ? launch_tiles<256, 256, 2, 4, 128, 2, kDirect>(g, s)
+                  : launch_tiles<256, 256, 2, 4, 128, 2, kStaged>(g, s);
   if (middle < small) {
-    if (!direct) return launch_tiles<128, 128, 2, 4, 128, 2, true>(g, s);
-    return tiles(128) <= cus ? launch_tiles<128, 128, 2, 4, 128, 4, false>(g, s)
-                             : launch_tiles<128, 128, 2, 2, 128, 2, false>(g, s);
+    if (!direct) return launch_tiles<128, 128, 2, 4, 128, 2, kStaged>(g, s);
+    return tiles(128) <= cus ? launch_tiles<128, 128, 2, 4, 128, 4, kDirect>(g, s)
+                             : launch_tiles<128, 128, 2, 2, 128, 2, kDirect>(g, s);
   }
-  return direct ? launch_tiles<64, 64, 2, 2, 128, 4, false>(g, s)
-                : launch_tiles<64, 64, 2, 2, 128, 2, true>(g, s);
+  return direct ? launch_tiles<64, 64, 2, 2, 128, 4, kDirect>(g, s)
+                : launch_tiles<64, 64, 2, 2, 128, 2, kStaged>(g, s);
 }
 
 }  // namespace repops

@@ -271,7 +271,10 @@ def test_quantize_rows_errs_by_half_a_step(rp):
 Q8_SHAPES = [(1, 1, 1), (1, 5, 0), (3, 2, 7), (1, 64, 64), (4, 1000, 4096), (16, 33, 100),
              (17, 129, 129), (31, 64, 1024), (33, 65, 63), (64, 64, 64), (65, 127, 999),
              (100, 300, 500), (128, 128, 128), (129, 257, 192), (333, 1001, 999), (256, 512, 4096),
-             (300, 1024, 48), (5, 4096, 14336), (40, 200, 30000), (513, 770, 640)]
+             (300, 1024, 48), (5, 4096, 14336), (40, 200, 30000), (513, 770, 640),
+             (100, 90, 15), (70, 70, 1), (200, 33, 16), (129, 70, 17), (40, 200, 5000),
+             (300, 64, 8192), (64, 1024, 4096), (1000, 100, 4096), (513, 300, 1500),
+             (1100, 1300, 333), (260, 5000, 270)]
 
 
 def codes(g, *shape):
