@@ -11,6 +11,12 @@
 // slice of BK codes of each row of a tile in chunks of 16, a row's chunks permuted
 // by its index so that eight neighbouring rows' reads of one chunk fall into
 // different banks.
+//
+// Bound: of many rows by the matrix units at the clock they hold (8192 x 14336, k
+// 4096: 453 us, 2.1 of the 2.25e15 operations a second that a large integer product of
+// the vendor's library reaches; 8192 x 4096, k 14336: 397 us, 2.4e15), of few by
+// reading B (4 x 32000, k 4096: 27.9 us, 4.7 TB/s), in between by the latency of a
+// slice and of the launch.
 #include <hip/hip_runtime.h>
 
 #include "generation_internal.h"

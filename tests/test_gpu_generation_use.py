@@ -331,3 +331,21 @@ def test_draw_past_2_31_logits(rp):
         assert_bits_equal(host(prob[at]), want[1])
         assert int(token.min()) >= 0
         del L
+
+
+def test_overlaps_are_refused_before_any_launch(rp):
+    import torch
+    x, r = torch.ones(8, 64, device="cuda:0"), torch.ones(8, 64, device="cuda:0")
+    q = torch.zeros(8, 64, dtype=torch.int8, device="cuda:0")
+    v = torch.ones(8, device="cuda:0")
+    announce("overlaps refused")
+    for call in (lambda: rp.add_rmsnorm_rows(x, r, sum_out=x, out=x),
+                 lambda: rp.add_rmsnorm_rows(x[:4], r[:4], sum_out=x[2:6]),
+                 lambda: rp.add_rmsnorm_quantize_rows(x, r, q_out=x.view(torch.int8)[:, :64]),
+                 lambda: rp.quantize_rows(x, q_out=x.view(torch.int8)[:, 64:128]),
+                 lambda: rp.add_rmsnorm_backward_rows(x, r, v, dgamma_out=r[0]),
+                 lambda: rp.matmul_q8(q, v, q, v, out=x[:, :8], bias=x[0, :8]),
+                 lambda: rp.sample_rows(x, v, prob_out=v)):
+        with pytest.raises(rp.RepopsError):
+            call()
+    assert (host(x) == 1).all() and (host(r) == 1).all() and (host(q) == 0).all() and (host(v) == 1).all()
