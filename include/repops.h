@@ -743,7 +743,8 @@ repops_status_t repops_matmul_q8(int64_t m, int64_t n, int64_t k, const int8_t *
                                  const float *b_scale, const float *bias, float *C, int64_t ldc,
                                  const repops_launch_t *launch, void *hip_stream);
 
-/* Workspace bytes of repops_sample_rows. */
+/* Workspace bytes of repops_sample_rows for exactly these sizes: 0 where a row takes one
+ * workgroup, and so not growing with the rows. */
 repops_status_t repops_sample_workspace(int64_t rows, int64_t vocab, uint64_t *bytes);
 
 /*

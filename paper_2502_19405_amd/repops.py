@@ -1062,7 +1062,7 @@ def matmul_q8(A: torch.Tensor, a_scale: torch.Tensor, B: torch.Tensor, b_scale: 
 
 
 def sample_workspace(rows: int, vocab: int) -> int:
-    """Bytes of workspace sample_rows needs."""
+    """Bytes of workspace sample_rows needs for exactly these sizes (few long rows; else 0)."""
     n = ctypes.c_uint64(0)
     _check((_lib or load()).repops_sample_workspace(rows, vocab, ctypes.byref(n)),
            "repops_sample_workspace")

@@ -155,6 +155,8 @@ def test_sample_rows_refusals():
     assert lib.repops_sample_workspace(4, 64, None) == rp.ERR_NULL
     with pytest.raises(rp.RepopsError):
         rp.sample_workspace(1, (1 << 20) + 1)
+    # only few long rows need one: a workspace for many rows is not one for few
+    assert rp.sample_workspace(300, 100000) == 0 == rp.sample_workspace(1, 40000)
     # bounded for any number of rows
     assert max(rp.sample_workspace(r, v) for r in (1, 1000, FAR) for v in (20000, 1 << 20)) <= 64 << 20
 
