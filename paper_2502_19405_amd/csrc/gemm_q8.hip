@@ -19,6 +19,8 @@
 // slice and of the launch.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "generation_internal.h"
 #include "repops_internal.h"
 #include "row_reduce.h"
@@ -490,24 +492,39 @@ __global__ __launch_bounds__(kFewWaves * 64) void q8_few_kernel(Q8Args g) {
           for (int t = 0; t < MT; ++t)
             acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(av[u][h][t], bv[u][h], acc[t], 0, 0, 0);
     }
-    for (; k0 < K; k0 += kStep) {
-      const int at = static_cast<int>(k0) + quarter * 32, end = static_cast<int>(K);
-      v4i bv[2], av[2][MT];
+    // What is left (at most U steps that may reach past K), with all its loads in flight.
+    auto rest = [&](auto steps) {
+      constexpr int N = decltype(steps)::value;
+      const int end = static_cast<int>(K), at = static_cast<int>(k0) + quarter * 32;
+      v4i bv[N][2], av[N][2][MT];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        bv[h] = load_raw<SHORT>(b, at + h * kChunk, end);
+      for (int u = 0; u < N; ++u)
 #pragma unroll
-        for (int t = 0; t < MT; ++t) av[h][t] = load_raw<SHORT>(a[t], at + h * kChunk, end);
-      }
+        for (int h = 0; h < 2; ++h) {
+          const int kk = at + u * static_cast<int>(kStep) + h * kChunk;
+          bv[u][h] = load_raw<SHORT>(b, kk, end);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const v4i bp = placed(bv[h], at + h * kChunk, end);
-#pragma unroll
-        for (int t = 0; t < MT; ++t) {
-          const v4i ap = live[t] ? placed(av[h][t], at + h * kChunk, end) : v4i{0, 0, 0, 0};
-          acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(ap, bp, acc[t], 0, 0, 0);
+          for (int t = 0; t < MT; ++t) av[u][h][t] = load_raw<SHORT>(a[t], kk, end);
         }
-      }
+#pragma unroll
+      for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int kk = at + u * static_cast<int>(kStep) + h * kChunk;
+          const v4i bp = placed(bv[u][h], kk, end);
+#pragma unroll
+          for (int t = 0; t < MT; ++t) {
+            const v4i ap = live[t] ? placed(av[u][h][t], kk, end) : v4i{0, 0, 0, 0};
+            acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(ap, bp, acc[t], 0, 0, 0);
+          }
+        }
+    };
+    if constexpr (SHORT) {
+      if (k0 < K) rest(std::integral_constant<int, 1>());
+    } else {
+      if (k0 + 2 * kStep < K) rest(std::integral_constant<int, U>());
+      else if (k0 + kStep < K) rest(std::integral_constant<int, 2>());
+      else if (k0 < K) rest(std::integral_constant<int, 1>());
     }
     // element r of a lane: row 4 (lane / 16) + r, column lane % 16
 #pragma unroll

@@ -164,8 +164,8 @@ __device__ __forceinline__ void ln_bwd_terms(const RowBwdArgs& a, const float* x
 
 // The gradient added to dX (RowBwdArgs::dS): none, one read as X and dY are, or one
 // read past the caches, which hold X and dY for their second reading; dS is read once.
-// Past the caches above 64 MB of matrices (4096 x 4096: 67 us against 75, dX alone 40
-// against 47; 4096 x 2048, 134 MB: 34.3 against 38.2), where smaller ones are slower
+// Past the caches above 64 MB of matrices (4096 x 4096: 58.5 us against 64.4, dX alone
+// 40 against 47; 4096 x 2048, 134 MB: 34.6 against 45.4), where smaller ones are slower
 // (4096 x 768, 50 MB: 16.4 against 15.2).
 enum { kNoAdd, kAdd, kAddOnce };
 
